@@ -208,6 +208,170 @@ pipo_status pipo_op_rope(uint16_t* q, uint16_t* k, const float* cos_sin, int64_t
  * head_dim / 2.  `out` holds n_pos * head_dim floats.  Errors: ARG. */
 pipo_status pipo_rope_table(const pipo_shape* shape, int32_t n_pos, float* out);
 
+/* --- batches of sequences of different lengths over a paged 4-bit KV cache ---
+ *
+ * Keys and values live in pages of `page_size` positions (16, 32, 64, 128 or
+ * 256), each page holding all n_kv_heads heads (head_dim 64 or 128) of its
+ * positions, 4 bits an element in groups of 64 with the recipe of
+ * PIPO_KV_INT4_G64.  Sequence i of n_seq keeps the positions p * page_size ..
+ * of its cache in page table[i * table_stride + p]; which pages are free is for
+ * the caller (or pipo_op_kv_pages_resize and its neighbours) to say.  Every
+ * layer has a pool of the same n_pages pages, the pools layer_bytes apart (a
+ * multiple of 16, at least n_pages * pipo_kv_page_bytes), and one table serves
+ * them all.  A page's bytes are in the order the kernels read fastest
+ * (kvpages.h); they are written by pipo_op_kv_pages_append and may be moved
+ * whole.  `pool` (16-byte aligned) and `table` are device pointers, the
+ * struct itself is read on the host during the call.
+ *
+ * Positions, sequences, pages and lengths come from device memory, where the
+ * host cannot check them.  No value of theirs makes a call read or write
+ * outside the arrays it was given: what a wrong one does is said at each
+ * call.
+ */
+typedef struct {
+  void* pool;
+  int64_t layer_bytes;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim, n_seq;
+} pipo_kv_pages;
+
+/* Bytes of a page of one layer, page_size * n_kv_heads * 9 head_dim / 8; 0 for
+ * a shape that is not supported (see above; 2^31 bytes or more). */
+int64_t pipo_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/*
+ * Per-head RMSNorm of q and k and their rotary positions in one pass, each row
+ * at a position of its own: with y = x / sqrt(mean(x^2) + eps) * gamma over a
+ * head's head_dim elements (q_gamma, k_gamma [head_dim] fp16; NULL: y = x),
+ * q_out = rotate(y) * q_scale and k_out = rotate(y), the rotation being
+ * pipo_op_rope's by row pos[m] of cos_sin [n_pos][head_dim/2][2]; in fp32,
+ * rounded once.  Row m of q starts at q + m * ldq and holds n_heads heads (k:
+ * ldk, n_kv_heads), so both may lie in the rows of a fused projection; q_out
+ * may be q with ldqo = ldq (k_out likewise), other overlaps are not allowed.
+ * A row whose position is negative or not below n_pos is left as it was
+ * (padding).  head_dim 64 or 128, else PIPO_ERR_UNSUPPORTED.  cos_sin is
+ * 4-byte aligned; rows on 16 bytes run fastest.
+ */
+pipo_status pipo_op_qk_norm_rope(const uint16_t* q, int64_t ldq, const uint16_t* k, int64_t ldk,
+                                 const uint16_t* q_gamma, const uint16_t* k_gamma,
+                                 const float* cos_sin, int64_t n_pos, const int32_t* pos,
+                                 uint16_t* q_out, int64_t ldqo, uint16_t* k_out, int64_t ldko,
+                                 int64_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                 float eps, float q_scale, void* stream);
+
+/*
+ * Rows of new keys and values into the pages of `layer`: row m of k and v
+ * (fp16, n_kv_heads * head_dim elements at k + m * ldk and v + m * ldv) becomes
+ * position pos[m] of sequence seq[m], quantized with the recipe of
+ * PIPO_KV_INT4_G64; elements are first clamped to +-57344 and NaN counts as
+ * 0, so that what the cache holds is finite.  A row is skipped where seq[m] is
+ * not in [0, n_seq), pos[m] is negative or past the table's row, or the table's
+ * entry is not a page.  No two rows of a call may name the same position of
+ * the same page (one of them, or a mixture, stays).
+ */
+pipo_status pipo_op_kv_pages_append(const pipo_kv_pages* cache, int32_t layer, const int32_t* seq,
+                                    const int32_t* pos, const uint16_t* k, int64_t ldk,
+                                    const uint16_t* v, int64_t ldv, int64_t M, void* stream);
+
+/* The reverse: position pos[m] of sequence seq[m] to row m of k and v, code *
+ * scale + min rounded once to fp16.  Rows that append would skip are left as
+ * they were. */
+pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, const int32_t* seq,
+                                  const int32_t* pos, uint16_t* k, int64_t ldk, uint16_t* v,
+                                  int64_t ldv, int64_t M, void* stream);
+
+/*
+ * Causal attention of each sequence's newest rows over its pages.  Rows
+ * q_start[i] .. q_start[i+1] - 1 of q (fp16, scaled, n_heads * head_dim
+ * elements at q + m * ldq; o and ldo alike) are the last positions of sequence
+ * i, whose keys 0 .. kv_len[i] - 1 (its own rows' included) are in the cache:
+ * with n rows, row j sits at position kv_len[i] - n + j and sees the keys up to
+ * that position.  q_start has n_seq + 1 entries that do not decrease.  Query
+ * head h reads key/value head h / (n_heads / n_kv_heads), any whole ratio.
+ * Every key and value is read as code * scale + min; softmax and sums in fp32,
+ * the output rounded once to fp16.
+ *
+ * M: rows of q and o; max_q, max_len: bounds of a sequence's rows and keys that
+ * the host knows (max_len at most table_stride * page_size).  A length above
+ * max_len counts as max_len, a start outside [0, M] as the nearer end, and rows
+ * of a sequence with more than max_q of them may be left unwritten.  Keys on
+ * an entry of the table that is not a page are not seen, a row that sees no
+ * key becomes 0, rows outside q_start[0] .. q_start[n_seq] - 1 are left as
+ * they were.
+ *
+ * Where there are few sequences their keys are split over workgroups, whose
+ * partials go to `workspace` (device, caller-owned, contents arbitrary, 4-byte
+ * aligned) of pipo_op_attn_pages_workspace_bytes bytes for a second kernel to
+ * merge in order; with less (or NULL) they are not split: the same result up
+ * to rounding.  Calls sharing a workspace must not overlap in time.  The
+ * order of all sums is fixed by the arguments of the call.
+ * n_heads and n_seq up to 65535, M * n_heads and max_q * n_heads below 2^31,
+ * max_len up to 2^30, else PIPO_ERR_UNSUPPORTED.
+ */
+pipo_status pipo_op_attn_pages(const pipo_kv_pages* cache, int32_t layer, const uint16_t* q,
+                               int64_t ldq, const int32_t* q_start, const int32_t* kv_len,
+                               uint16_t* o, int64_t ldo, int32_t n_heads, int64_t M, int32_t max_q,
+                               int32_t max_len, void* workspace, int64_t workspace_bytes,
+                               void* stream);
+/* (pool and table of `cache` are not read; 0 for a call that would be refused
+ * or never splits) */
+int64_t pipo_op_attn_pages_workspace_bytes(const pipo_kv_pages* cache, int32_t n_heads, int64_t M,
+                                           int32_t max_q, int32_t max_len);
+
+/*
+ * Page tables.  A sequence of len[i] tokens holds the first ceil(len[i] /
+ * page_size) entries of its row (a negative length counts as 0), a page that
+ * no row holds is free, and the same page may be in several rows (a shared
+ * prefix).  The calls read a table [n_seq][table_stride] and lengths and write
+ * the next ones, whose entries past a row's pages become -1.  resize and
+ * compact may work in place (table_out = table, len_out = len); any other
+ * overlap of an output with another array is PIPO_ERR_ARG.  Up to 2048
+ * sequences, 2^20 pages and 2^31 - 1 table entries (else PIPO_ERR_UNSUPPORTED);
+ * one workgroup does the work, so a captured decode loop can grow its
+ * sequences without the host.
+ *
+ * resize: sequence i gets want[i] tokens (negative: it keeps its length).
+ * Pages past ceil(want[i] / page_size) are given up, missing ones are the lowest
+ * free pages (those given up in this call included), in order of the
+ * sequences.  want[i] = 0 frees a sequence.  If there are too few pages, or a
+ * row is too short, the table and lengths stay what they were and *missing
+ * (device) is how many pages were lacking, else 0.
+ */
+pipo_status pipo_op_kv_pages_resize(const int32_t* table, const int32_t* len, const int32_t* want,
+                                    int32_t* table_out, int32_t* len_out, int64_t table_stride,
+                                    int32_t n_seq, int32_t n_pages, int32_t page_size,
+                                    int32_t* missing, void* stream);
+
+/*
+ * fork: sequence i < n_out of the output continues sequence parent[i] of the
+ * input (outside [0, n_seq): it is empty).  Children share their parent's full
+ * pages; a last page with room left stays with the parent's first child, and
+ * each other child gets the lowest free page (free in the output, in order of
+ * the children) and a pair (old page, new page) in `pairs` [n_out][2], for
+ * pipo_op_kv_pages_copy.  *n_pairs and *missing are device counts; with
+ * *missing > 0 pages lacking, *n_pairs is 0 and nothing else is written.
+ */
+pipo_status pipo_op_kv_pages_fork(const int32_t* table, const int32_t* len, int32_t n_seq,
+                                  const int32_t* parent, int32_t* table_out, int32_t* len_out,
+                                  int32_t n_out, int64_t table_stride, int32_t n_pages,
+                                  int32_t page_size, int32_t* pairs, int32_t* n_pairs,
+                                  int32_t* missing, void* stream);
+
+/* compact: with U pages in use, those at U and above move, in order, to the
+ * pages below U that are free; pairs [n_pages / 2][2] and *n_pairs say which
+ * (old page, new page), for pipo_op_kv_pages_copy. */
+pipo_status pipo_op_kv_pages_compact(const int32_t* table, const int32_t* len, int32_t* table_out,
+                                     int64_t table_stride, int32_t n_seq, int32_t n_pages,
+                                     int32_t page_size, int32_t* pairs, int32_t* n_pairs,
+                                     void* stream);
+
+/* Page pairs[i][0] onto page pairs[i][1] in every layer, for i below *n_pairs
+ * (device; at most max_pairs count).  Pairs with an entry that is not a page
+ * are skipped; a page that is written may be in no other pair. */
+pipo_status pipo_op_kv_pages_copy(const pipo_kv_pages* cache, const int32_t* pairs,
+                                  const int32_t* n_pairs, int32_t max_pairs, void* stream);
+
 /* SwiGLU: h[m][i] = silu(gu[m][i]) * gu[m][F + i], silu(g) = g / (1 +
  * exp(-g)), in fp32; gu [M][2F], h [M][F] fp16, F % 8 == 0. */
 pipo_status pipo_op_swiglu(const uint16_t* gu, uint16_t* h, int64_t M, int64_t F, void* stream);

@@ -31,3 +31,4 @@ from .llama import (  # noqa: F401
     rope_frequencies,
     swiglu,
 )
+from . import pages  # noqa: F401

@@ -98,6 +98,12 @@ class PipoStats(ctypes.Structure):
                 ("kernels", PipoKernelStat * PIPO_MAX_KERNEL_STATS)]
 
 
+class PipoKvPages(ctypes.Structure):
+    _fields_ = [("pool", vp), ("layer_bytes", i64), ("table", vp), ("table_stride", i64),
+                ("n_layers", i32), ("n_pages", i32), ("page_size", i32), ("n_kv_heads", i32),
+                ("head_dim", i32), ("n_seq", i32)]
+
+
 class PipoSchedConfig(ctypes.Structure):
     _fields_ = [("n_layers", i32), ("n_slots", i32), ("n_h2d", i32), ("layers_streamed", i32),
                 ("head_streamed", i32), ("kv_on_host", i32), ("poison", i32), ("delay", i32),
@@ -168,6 +174,20 @@ _SIGNATURES = {
     "pipo_op_rmsnorm": ([vp, vp, vp, i64, i64, i64, i64, f32, vp], i32),
     "pipo_op_rope": ([vp, vp, vp, i64, i64, i64, i64, i64, i32, i32, i32, f32, vp], i32),
     "pipo_rope_table": ([ctypes.POINTER(PipoShape), i32, vp], i32),
+    "pipo_kv_page_bytes": ([i32, i32, i32], i64),
+    "pipo_op_qk_norm_rope": ([vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, i64, i64, i32,
+                              i32, i32, f32, f32, vp], i32),
+    "pipo_op_kv_pages_append": ([ctypes.POINTER(PipoKvPages), i32, vp, vp, vp, i64, vp, i64, i64,
+                                 vp], i32),
+    "pipo_op_kv_pages_read": ([ctypes.POINTER(PipoKvPages), i32, vp, vp, vp, i64, vp, i64, i64,
+                               vp], i32),
+    "pipo_op_attn_pages": ([ctypes.POINTER(PipoKvPages), i32, vp, i64, vp, vp, vp, i64, i32, i64,
+                            i32, i32, vp, i64, vp], i32),
+    "pipo_op_attn_pages_workspace_bytes": ([ctypes.POINTER(PipoKvPages), i32, i64, i32, i32], i64),
+    "pipo_op_kv_pages_resize": ([vp, vp, vp, vp, vp, i64, i32, i32, i32, vp, vp], i32),
+    "pipo_op_kv_pages_fork": ([vp, vp, i32, vp, vp, vp, i32, i64, i32, i32, vp, vp, vp, vp], i32),
+    "pipo_op_kv_pages_compact": ([vp, vp, vp, i64, i32, i32, i32, vp, vp, vp], i32),
+    "pipo_op_kv_pages_copy": ([ctypes.POINTER(PipoKvPages), vp, vp, i32, vp], i32),
     "pipo_op_swiglu": ([vp, vp, i64, i64, vp], i32),
     "pipo_op_embed": ([vp, vp, vp, vp, i64, i64, i64, i64, i64, vp], i32),
     "pipo_sched_trace": ([ctypes.POINTER(PipoSchedConfig), i32, vp, vp, vp, i64, vp, i64], i64),
@@ -531,6 +551,66 @@ def pipo_rope_table(shape: PipoShape, n_pos: int) -> np.ndarray:
     out = np.zeros((n_pos, dh // 2, 2), dtype=np.float32)
     _check(lib().pipo_rope_table(ctypes.byref(shape), n_pos, _ptr(out)), "pipo_rope_table")
     return out
+
+
+# --- batches over a paged 4-bit KV cache ---
+def pipo_kv_page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().pipo_kv_page_bytes(page_size, n_kv_heads, head_dim))
+
+
+def pipo_op_qk_norm_rope(q, ldq, k, ldk, q_gamma, k_gamma, cos_sin, n_pos, pos, q_out, ldqo, k_out,
+                         ldko, M, n_heads, n_kv_heads, head_dim, eps, q_scale, stream=None):
+    _check(lib().pipo_op_qk_norm_rope(q, ldq, k, ldk, q_gamma, k_gamma, cos_sin, n_pos, pos, q_out,
+                                      ldqo, k_out, ldko, M, n_heads, n_kv_heads, head_dim, eps,
+                                      q_scale, stream), "pipo_op_qk_norm_rope")
+
+
+def pipo_op_kv_pages_append(cache: PipoKvPages, layer, seq, pos, k, ldk, v, ldv, M, stream=None):
+    _check(lib().pipo_op_kv_pages_append(ctypes.byref(cache), layer, seq, pos, k, ldk, v, ldv, M,
+                                         stream), "pipo_op_kv_pages_append")
+
+
+def pipo_op_kv_pages_read(cache: PipoKvPages, layer, seq, pos, k, ldk, v, ldv, M, stream=None):
+    _check(lib().pipo_op_kv_pages_read(ctypes.byref(cache), layer, seq, pos, k, ldk, v, ldv, M,
+                                       stream), "pipo_op_kv_pages_read")
+
+
+def pipo_op_attn_pages(cache: PipoKvPages, layer, q, ldq, q_start, kv_len, o, ldo, n_heads, M, max_q,
+                       max_len, workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().pipo_op_attn_pages(ctypes.byref(cache), layer, q, ldq, q_start, kv_len, o, ldo,
+                                    n_heads, M, max_q, max_len, workspace, workspace_bytes, stream),
+           "pipo_op_attn_pages")
+
+
+def pipo_op_attn_pages_workspace_bytes(cache: PipoKvPages, n_heads, M, max_q, max_len) -> int:
+    return int(lib().pipo_op_attn_pages_workspace_bytes(ctypes.byref(cache), n_heads, M, max_q,
+                                                        max_len))
+
+
+def pipo_op_kv_pages_resize(table, length, want, table_out, len_out, table_stride, n_seq, n_pages,
+                            page_size, missing, stream=None):
+    _check(lib().pipo_op_kv_pages_resize(table, length, want, table_out, len_out, table_stride,
+                                         n_seq, n_pages, page_size, missing, stream),
+           "pipo_op_kv_pages_resize")
+
+
+def pipo_op_kv_pages_fork(table, length, n_seq, parent, table_out, len_out, n_out, table_stride,
+                          n_pages, page_size, pairs, n_pairs, missing, stream=None):
+    _check(lib().pipo_op_kv_pages_fork(table, length, n_seq, parent, table_out, len_out, n_out,
+                                       table_stride, n_pages, page_size, pairs, n_pairs, missing,
+                                       stream), "pipo_op_kv_pages_fork")
+
+
+def pipo_op_kv_pages_compact(table, length, table_out, table_stride, n_seq, n_pages, page_size,
+                             pairs, n_pairs, stream=None):
+    _check(lib().pipo_op_kv_pages_compact(table, length, table_out, table_stride, n_seq, n_pages,
+                                          page_size, pairs, n_pairs, stream),
+           "pipo_op_kv_pages_compact")
+
+
+def pipo_op_kv_pages_copy(cache: PipoKvPages, pairs, n_pairs, max_pairs, stream=None):
+    _check(lib().pipo_op_kv_pages_copy(ctypes.byref(cache), pairs, n_pairs, max_pairs, stream),
+           "pipo_op_kv_pages_copy")
 
 
 def pipo_op_swiglu(gu, h, M, F, stream=None):

@@ -14,26 +14,9 @@
 // in a row, took 6 us for 128 rows of 7168, about 2 more than a launch.)
 #include "common.h"
 #include "device.h"
+#include "kvquant.h"
 
 namespace pipo {
-
-// largest of the 8 lanes of a group, by DPP moves within a row of 16 lanes
-// (swap neighbours, swap pairs, mirror within 8)
-template <int CTRL>
-__device__ __forceinline__ float lane_move(float v) {
-  return __uint_as_float(
-      __builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xF, 0xF, false));
-}
-__device__ __forceinline__ float group_max8(float v) {
-  v = fmaxf(v, lane_move<0xB1>(v));
-  v = fmaxf(v, lane_move<0x4E>(v));
-  return fmaxf(v, lane_move<0x141>(v));
-}
-__device__ __forceinline__ float group_min8(float v) {
-  v = fminf(v, lane_move<0xB1>(v));
-  v = fminf(v, lane_move<0x4E>(v));
-  return fminf(v, lane_move<0x141>(v));
-}
 
 // row and 8-element piece of this thread; false past the end.  A row has a
 // multiple of 32 pieces, so the 8 lanes of a group are all in or all out.
@@ -61,38 +44,18 @@ __global__ __launch_bounds__(256) void kv_quant_k(const uint16_t* __restrict__ x
   int c;  // 8-element piece of row r
   if (!piece_of(rows, d, r, c)) return;
   const h8 h = load_h8(x + r * d + 8 * c);
-  float v[8], mn, mx;
+  float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
-  mn = mx = v[0];
-#pragma unroll
-  for (int j = 1; j < 8; ++j) {
-    mn = fminf(mn, v[j]);
-    mx = fmaxf(mx, v[j]);
-  }
-  mn = group_min8(mn);
-  mx = group_max8(mx);
-  const _Float16 s16 = (_Float16)((mx - mn) / 15.f);
-  const _Float16 m16 = (_Float16)mn;
-  const float s = (float)s16, m = (float)m16;
-  // (x - min) / scale, correctly rounded from the correctly rounded reciprocal
-  // and one residual step (Markstein, IBM J. Res. Dev. 34, 1990): an eighth of
-  // a division per element.  Infinite inputs give NaN and code 0, as the
-  // division would.
-  const float inv = s != 0.f ? 1.f / s : 0.f;
+  const Quant8 q = quantize8(v);
   uint32_t word = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float x = v[j] - m, q0 = x * inv;
-    const float q = __builtin_fmaf(__builtin_fmaf(-q0, s, x), inv, q0);
-    word |= (uint32_t)(s != 0.f ? fminf(fmaxf(__builtin_rintf(q), 0.f), 15.f) : 0.f) << (4 * j);
-  }
+  for (int j = 0; j < 8; ++j) word |= q.c[j] << (4 * j);
   uint8_t* row = out + r * (d / 2 + d / 16);
   *reinterpret_cast<uint32_t*>(row + 4 * c) = word;
   if (c % 8 == 0)
     *reinterpret_cast<uint32_t*>(row + d / 2 + c / 8 * 4) =
-        (uint32_t)__builtin_bit_cast(uint16_t, s16) |
-        ((uint32_t)__builtin_bit_cast(uint16_t, m16) << 16);
+        (uint32_t)q.scale | ((uint32_t)q.min << 16);
 }
 
 __global__ __launch_bounds__(256) void kv_dequant_k(const uint8_t* __restrict__ in,

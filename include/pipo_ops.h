@@ -301,7 +301,7 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  * they were.
  *
  * Where there are few sequences their keys are split over workgroups, whose
- * partials go to `workspace` (device, caller-owned, contents arbitrary, 4-byte
+ * partials go to `workspace` (device, caller-owned, contents arbitrary, 16-byte
  * aligned) of pipo_op_attn_pages_workspace_bytes bytes for a second kernel to
  * merge in order; with less (or NULL) they are not split: the same result up
  * to rounding.  Calls sharing a workspace must not overlap in time.  The

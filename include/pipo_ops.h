@@ -306,8 +306,9 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  * merge in order; with less (or NULL) they are not split: the same result up
  * to rounding.  Calls sharing a workspace must not overlap in time.  The
  * order of all sums is fixed by the arguments of the call.
- * n_heads and n_seq up to 65535, M * n_heads and max_q * n_heads below 2^31,
- * max_len up to 2^30, else PIPO_ERR_UNSUPPORTED.
+ * n_heads and n_seq up to 65535, n_seq * n_kv_heads below 2^22, max_len up to
+ * 2^30, min(M, max_q) * n_heads up to 2^29 - 2^22 and M * n_heads below 2^31,
+ * else PIPO_ERR_UNSUPPORTED.
  */
 pipo_status pipo_op_attn_pages(const pipo_kv_pages* cache, int32_t layer, const uint16_t* q,
                                int64_t ldq, const int32_t* q_start, const int32_t* kv_len,

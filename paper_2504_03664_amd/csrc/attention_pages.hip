@@ -28,12 +28,15 @@ struct AttnPages {
   float2* part_rl;
   int64_t ldq, ldo, M;
   int H, G, max_q, max_len;
-  int chunk;                  // keys of a split
+  int chunk_few, chunk_many;  // keys of a split, by the sequence's columns
   int splits;                 // of a row's partials in `part`
   bool q_vec, o_vec;          // q rows 16-byte aligned, o rows 8-byte
 };
 
-constexpr int kBlockKeys = 32;
+// Up to this many columns a sequence is attn_pages_few_k's, above it
+// attn_pages_many_k's.
+constexpr int kFewCols = 64;
+constexpr int kBlockKeys = 32;  // of attn_pages_few_k
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^15 / (a bound of the values' scales), so that p s fits a half
@@ -122,6 +125,22 @@ __device__ __forceinline__ void issue_tile(const uint8_t* tile, uint8_t* lds, in
 template <int D>
 constexpr int kTileLoads = D / 64 + 1;
 
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint8_t* p) {
+  if constexpr (N == 2) {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    w[0] = x[0];
+    w[1] = x[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p + 16 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = x[j];
+    }
+  }
+}
+
 // what a lane holds of two tiles' keys (or values): operand words of codes, and
 // the pairs of keys 4 g .. 4 g + 3
 template <int D>
@@ -196,19 +215,18 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
   }
 }
 
-// A workgroup is W waves on (sequence, key/value head, 16 columns,
+// Few columns: a workgroup is W waves on (sequence, key/value head, 16 columns,
 // split) that take the split's keys by turns, 32 at a time, from the cache into
 // operand registers.
 template <int D, int W>
 __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(3))) void
-attn_pages_k(AttnPages a) {
+attn_pages_few_k(AttnPages a) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16;
-  const int kh = blockIdx.x % a.c.Hkv, ct = blockIdx.x / a.c.Hkv, sp = blockIdx.y;
-  const int si = blockIdx.z;
+  const int kh = blockIdx.x % a.c.Hkv, si = blockIdx.x / a.c.Hkv, sp = blockIdx.y, ct = blockIdx.z;
   const Seq s = sequence(a, si);
   const int cols = s.nq * a.G;
-  if (16 * ct >= cols) return;
-  const int ns = max(1, (s.len + a.chunk - 1) / a.chunk);
+  if (16 * ct >= cols || cols > kFewCols) return;
+  const int ns = max(1, (s.len + a.chunk_few - 1) / a.chunk_few);
   if (sp >= ns) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -228,7 +246,7 @@ attn_pages_k(AttnPages a) {
   const int jmin = 16 * ct / a.G, jmax = min(s.nq - 1, (16 * ct + 15) / a.G);
   const int all = max(0, s.len - s.nq + jmin + 1);      // visible to every column
   const int end = max(0, s.len - s.nq + jmax + 1);      // to any
-  const int p0 = sp * a.chunk, p1 = min(end, p0 + a.chunk);
+  const int p0 = sp * a.chunk_few, p1 = min(end, p0 + a.chunk_few);
 
   f4 acc[NF];
 #pragma unroll
@@ -267,7 +285,8 @@ attn_pages_k(AttnPages a) {
   if (p + step < p1) issue(p + step, 1);
 
   h8 qf[KK];
-  float qsum[NG], qbias[NG];  // of the column's q, and times the codes' bias
+  float qsum[NG];  // of the column's q
+  f4 init[NG];     // less q times the codes' bias
 #pragma unroll
   for (int n = 0; n < NG; ++n) {
     float bias = 0.f, sum = 0.f;
@@ -281,7 +300,8 @@ attn_pages_k(AttnPages a) {
       }
     }
     qsum[n] = cols_sum(sum);
-    qbias[n] = cols_sum(bias);
+    bias = cols_sum(bias);
+    init[n] = f4{-bias, -bias, -bias, -bias};
   }
 
   const auto compute = [&](int p, int slot, auto edge_c) {
@@ -298,7 +318,7 @@ attn_pages_k(AttnPages a) {
       f4 sc[NG];
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        sc[n] = mfma16(k_codes(t.c[j][2 * n], mg), qf[2 * n], f4{0.f, 0.f, 0.f, 0.f});
+        sc[n] = mfma16(k_codes(t.c[j][2 * n], mg), qf[2 * n], init[n]);
         sc[n] = mfma16(k_codes(t.c[j][2 * n + 1], mg), qf[2 * n + 1], sc[n]);
       }
 #pragma unroll
@@ -308,7 +328,7 @@ attn_pages_k(AttnPages a) {
         for (int n = 0; n < NG; ++n) {
           const uint32_t w = t.pair[j][e * NG + n];
           v = n == 0 ? lo_half(w) * qsum[0] : __builtin_fmaf(lo_half(w), qsum[n], v);
-          v = __builtin_fmaf(hi_half(w), sc[n][e] - qbias[n], v);
+          v = __builtin_fmaf(hi_half(w), sc[n][e], v);
         }
         if constexpr (EDGE) {
           const int key = 4 * g + e;
@@ -359,11 +379,11 @@ attn_pages_k(AttnPages a) {
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
           const uint32_t w = t.pair[j][e * NG + n];
-          // p s in two halves, 22 bits of it
-          const float ys = y * hi_half(w);
-          const _Float16 a16 = (_Float16)ys;
+          // p s in two halves, 22 bits of it (fused, so that each is one
+          // instruction with its rounding)
+          const _Float16 a16 = (_Float16)__builtin_fmaf(y, hi_half(w), 0.f);
           hi[n][4 * j + kOrder[e]] = a16;
-          lo[n][4 * j + kOrder[e]] = (_Float16)(ys - (float)a16);
+          lo[n][4 * j + kOrder[e]] = (_Float16)__builtin_fmaf(y, hi_half(w), -(float)a16);
           msum[n] = __builtin_fmaf(y, lo_half(w), msum[n]);
         }
       }
@@ -436,6 +456,357 @@ attn_pages_k(AttnPages a) {
   }
 }
 
+// Many columns: a workgroup is four waves of 32 columns each on (sequence,
+// key/value head, 128 columns, split).  They take the split's keys 64 at a time:
+// each wave unpacks a tile of the next block into LDS, in operand order (keys as c,
+// values as c - 7.5), while all of them work on this one, so a block is unpacked once for 128
+// columns and every LDS access is a wave's contiguous kilobyte.  The weights p s
+// go to the second product rounded to a half: with the codes centred, and the
+// rest of a value, p (m + 7.5 s), summed in fp32, that is one rounding of the
+// size of the output's own.
+constexpr int kManyCols = 128, kManyKeys = 64;
+
+// a word of K codes -> eight dimensions, c
+__device__ __forceinline__ h8 k_plain(uint32_t w, const Magic& g) {
+  const h8 bias = {256.f16, 256.f16, 16.f16, 16.f16, 256.f16, 256.f16, 16.f16, 16.f16};
+  return k_codes(w, g) - bias;
+}
+// a V word -> four keys (0, 2, 1, 3) of dimension 32 w + r (half 0) or 32 w + 16
+// + r, c - 7.5
+template <int HALF>
+__device__ __forceinline__ h4 v_centred(uint32_t w, const Magic& g) {
+  const uint32_t m = HALF ? g.m16 : g.m256, e = HALF ? g.e16 : g.e256;
+  u32x2 o;
+  o[0] = ((w << 2) & m) | e;
+  o[1] = ((w >> 6) & m) | e;
+  constexpr _Float16 b = HALF ? 23.5f16 : 263.5f16;
+  return __builtin_bit_cast(h4, o) - h4{b, b, b, b};
+}
+
+// Sequence at place z of the launch: up to 64 sequences go by their keys, the most
+// first (16 prompts' 509 rows each over 509 to 4099 keys: 556 -> 489 us).
+__device__ __forceinline__ int seq_in_order(const AttnPages& a, int z) {
+  const int n = a.c.n_seq, lane = threadIdx.x & 63;
+  if (n == 1 || n > 64) return z;
+  const int keys = lane < n ? a.kv_len[lane] : 0;
+  int rank = 0;
+  for (int i = 0; i < n; ++i) {
+    const int k = __builtin_amdgcn_readlane(keys, i);
+    rank += k > keys || (k == keys && i < lane);
+  }
+  return __ffsll((unsigned long long)__ballot(lane < n && rank == z)) - 1;
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move_u(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false);
+}
+
+// Makes the compiler forget that it has converted these halves, so that the next
+// use takes them as operands of a mixed multiply-add instead of as floats kept in
+// registers.
+template <int N>
+__device__ __forceinline__ void as_halves(uint32_t (&w)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i]));
+}
+
+template <int D>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void
+attn_pages_many_k(AttnPages a) {
+  constexpr int KK = D / 32, NG = D / 64, NF = D / 16, T = kManyKeys / 16, U = 2;
+  const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y, si = seq_in_order(a, blockIdx.z);
+  const Seq s = sequence(a, si);
+  const int cols = s.nq * a.G;
+  if (cols <= kFewCols) return;
+  // the tiles with the most keys first
+  const int ct = (int)(gridDim.x / a.c.Hkv) - 1 - (int)(blockIdx.x / a.c.Hkv);
+  if (kManyCols * ct >= cols) return;
+  const int ns = max(1, (s.len + a.chunk_many - 1) / a.chunk_many);
+  if (sp >= ns) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const Magic mg = magic();
+
+  // K operands [tile][kk][lane], V operands [pair of tiles][fragment][lane], the
+  // (min, scale) words [K, V][tile][key][group] (0 past the end), the largest of
+  // each tile's V and which tiles are pages'
+  struct Stage {
+    h8 k[T][KK][64];
+    h8 v[T / 2][NF][64];
+    uint32_t pair[2][T][16 * NG];
+    uint32_t top[T], valid[T];
+  };
+  __shared__ Stage st[2];
+
+  const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
+  const int q_last = min(s.nq - 1, (kManyCols * ct + kManyCols - 1) / a.G);
+  const int end = max(0, s.len - s.nq + q_last + 1);  // keys visible to any column
+  const int p0 = sp * a.chunk_many, p1 = min(end, p0 + a.chunk_many);
+  const int blocks = p1 > p0 ? (p1 - p0 + kManyKeys - 1) / kManyKeys : 0;
+  // keys visible to all of the wave's columns, and to any
+  const int all = max(0, s.len - s.nq + c0 / a.G + 1);
+  const int end_w = c0 < cols ? min(p1, s.len - s.nq + min(s.nq - 1, (c0 + 31) / a.G) + 1) : 0;
+
+  // this wave's tile of the next block, on its way
+  uint32_t kw[KK], vw[KK];
+  u32x4 pw;
+  uint32_t ok;
+  int lim;
+  // lane i holds the page of its tile in block i, 64 blocks at a time
+  const int32_t* row = a.c.table + si * a.c.stride;
+  int pages = -1;
+  const auto fetch = [&](int blk) {
+    const int pos = p0 + blk * kManyKeys + 16 * wave;
+    if ((blk & 63) == 0) {
+      const int64_t at = (int64_t)pos + (int64_t)lane * kManyKeys;
+      pages = at < p1 ? row[at >> a.c.ps_log2] : -1;
+    }
+    lim = p1 - pos;
+    const int page = __builtin_amdgcn_readlane(pages, blk & 63);
+    ok = page >= 0 && page < a.c.n_pages;
+    const uint8_t* tile = tile_at<D>(a.c, ok ? page : 0, kh, pos);
+    load_words(kw, tile + lane * (D / 8));
+    load_words(vw, tile + 8 * D + lane * (D / 8));
+    if (lane < D / 8) pw = *reinterpret_cast<const u32x4*>(tile + 16 * D + 16 * lane);
+  };
+  const auto unpack = [&](Stage& x) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) x.k[wave][kk][lane] = k_plain(kw[kk], mg);
+#pragma unroll
+    for (int w = 0; w < KK; ++w) {
+      h4* v0 = reinterpret_cast<h4*>(&x.v[wave / 2][2 * w][lane]);
+      h4* v1 = reinterpret_cast<h4*>(&x.v[wave / 2][2 * w + 1][lane]);
+      v0[wave % 2] = v_centred<0>(vw[w], mg);
+      v1[wave % 2] = v_centred<1>(vw[w], mg);
+    }
+    if (lane < D / 8) {  // the first half of these lanes has K's, the others V's
+      const int at = 4 * (lane % (D / 16));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if ((at + i) / NG >= lim) pw[i] = 0;  // past the end: anything
+      *reinterpret_cast<u32x4*>(x.pair[lane / (D / 16)][wave] + at) = pw;
+      uint32_t top = max(max(pw[0], pw[1]), max(pw[2], pw[3]));
+      top = max(top, lane_move_u<0xB1>(top));
+      top = max(top, lane_move_u<0x4E>(top));
+      if constexpr (D == 128) top = max(top, lane_move_u<0x141>(top));
+      if (lane == D / 16) {
+        x.top[wave] = top;
+        x.valid[wave] = ok;
+      }
+    }
+  };
+
+  h8 qf[U][KK];
+  float qsum[U][NG];
+  int vis[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int col = c0 + 16 * u + r, qj = col / a.G;
+    vis[u] = col < cols ? max(0, s.len - s.nq + qj + 1) : 0;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      float sum = 0.f;
+#pragma unroll
+      for (int kk = 2 * n; kk < 2 * n + 2; ++kk) {
+        qf[u][kk] = col < cols ? load_q<D>(a, s.row0 + qj, kh * a.G + col % a.G, 32 * kk + 8 * g)
+                               : zero_h8();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += (float)qf[u][kk][j];
+      }
+      qsum[u][n] = cols_sum(sum);
+    }
+  }
+  f4 acc[U][NF];
+  float R[U], l[U], msum[U][NG];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    R[u] = -INFINITY;
+    l[u] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NG; ++n) msum[u][n] = 0.f;
+#pragma unroll
+    for (int n = 0; n < NF; ++n) acc[u][n] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const auto compute = [&](const Stage& x, int k0, auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+    float sc[U][T][4];
+    h8 kf[2][KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kf[0][kk] = x.k[0][kk][lane];
+#pragma unroll
+    for (int j = 0; j < T; ++j) {
+      f4 d[U][NG];
+      uint32_t w[4 * NG];
+      load_words(w, reinterpret_cast<const uint8_t*>(&x.pair[0][j][4 * g * NG]));
+      if (j + 1 < T) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[(j + 1) & 1][kk] = x.k[j + 1][kk][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (these loads travel beside this tile's work)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          d[u][kk / 2] =
+              mfma16(kf[j & 1][kk], qf[u][kk], kk % 2 ? d[u][kk / 2] : f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u > 0) as_halves(w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float v = 0.f;
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            v = n == 0 ? lo_half(w[e * NG]) * qsum[u][0]
+                       : __builtin_fmaf(lo_half(w[e * NG + n]), qsum[u][n], v);
+            v = __builtin_fmaf(hi_half(w[e * NG + n]), d[u][n][e], v);
+          }
+          if constexpr (EDGE) v = x.valid[j] && k0 + 16 * j + 4 * g + e < vis[u] ? v : -INFINITY;
+          sc[u][j][e] = v;
+        }
+      }
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < T; ++j) top = max(top, x.top[j]);
+    // scales are below 2^(exponent field - 14)
+    const float es = (float)((int)(top >> 26) - 14);
+    float shift[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float bm = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bm = fmaxf(bm, sc[u][j][e]);
+      bm = cols_max(bm);
+      const float Rn = fmaxf(R[u], __builtin_fmaf(bm, kLog2e, es));
+      const float Rs = EDGE && Rn == -INFINITY ? 0.f : Rn;
+      const float alpha = __builtin_amdgcn_exp2f(R[u] - Rs);
+      R[u] = Rn;
+      shift[u] = kPBits - Rs;
+      if (__any(alpha != 1.f)) {
+        l[u] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) msum[u][n] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NF; ++n) acc[u][n] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < T / 2; ++t) {
+      h8 pf[U][NG];
+      uint32_t vp[2][4 * NG];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+        load_words(vp[jj], reinterpret_cast<const uint8_t*>(&x.pair[1][2 * t + jj][4 * g * NG]));
+      h8 vf[NF];
+#pragma unroll
+      for (int n = 0; n < NF; ++n) vf[n] = x.v[t][n][lane];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          constexpr int kOrder[4] = {0, 2, 1, 3};  // of v_centred
+          const int j = 2 * t + jj;
+          float y[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            y[u] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][j][e], kLog2e, shift[u]));
+            l[u] += y[u];
+          }
+#pragma unroll
+          for (int n = 0; n < NG; ++n) {
+            uint32_t w[1] = {vp[jj][e * NG + n]};
+            const float mu = __builtin_fmaf(hi_half(w[0]), 7.5f, lo_half(w[0]));
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              as_halves(w);
+              pf[u][n][4 * jj + kOrder[e]] = (_Float16)__builtin_fmaf(y[u], hi_half(w[0]), 0.f);
+              msum[u][n] = __builtin_fmaf(y[u], mu, msum[u][n]);
+            }
+          }
+        }
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) acc[u][n] = mfma16(vf[n], pf[u][n / 4], acc[u][n]);
+      }
+    }
+  };
+
+  if (blocks > 0) {
+    fetch(0);
+    unpack(st[0]);
+  }
+  __syncthreads();
+  int blk = 0;
+  // first the blocks that all columns of the wave see whole, up to one with a
+  // tile that is no page's; every wave goes through every block
+  const auto run = [&](auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+    for (; blk < blocks; ++blk) {
+      const Stage& x = st[blk & 1];
+      const int k0 = p0 + blk * kManyKeys;
+      if constexpr (!EDGE) {
+        uint32_t v = 1;
+#pragma unroll
+        for (int j = 0; j < T; ++j) v &= x.valid[j];
+        if (k0 + kManyKeys > all || !__builtin_amdgcn_readfirstlane(v)) return;
+      }
+      if (blk + 1 < blocks) fetch(blk + 1);
+      if (!EDGE || k0 < end_w) compute(x, k0, edge_c);
+      if (blk + 1 < blocks) unpack(st[(blk + 1) & 1]);
+      __syncthreads();
+    }
+  };
+  run(std::false_type{});
+  run(std::true_type{});
+
+  // element e of acc[u][n]: dimension 16 n + 4 g + e of column c0 + 16 u + r
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int col = c0 + 16 * u + r;
+    const float L = cols_sum(l[u]);
+    float ms[NG];
+#pragma unroll
+    for (int n = 0; n < NG; ++n) ms[n] = cols_sum(msum[u][n]);
+    if (col >= cols) continue;
+    const int m = s.row0 + col / a.G, h = kh * a.G + col % a.G;
+    if (ns == 1) {
+      const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+      uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        uint16_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f2h((acc[u][n][e] + ms[n / 4]) * inv);
+        if (a.o_vec) {
+          *reinterpret_cast<u32x2*>(o + 16 * n + 4 * g) =
+              u32x2{(uint32_t)v[0] | ((uint32_t)v[1] << 16), (uint32_t)v[2] | ((uint32_t)v[3] << 16)};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[16 * n + 4 * g + e] = v[e];
+        }
+      }
+    } else {
+      const int64_t at = ((int64_t)m * a.H + h) * a.splits + sp;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        f4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[u][n][e] + ms[n / 4];
+        *reinterpret_cast<f4*>(a.part + at * D + 16 * n + 4 * g) = v;
+      }
+      if (g == 0) a.part_rl[at] = make_float2(R[u], L);
+    }
+  }
+}
+
 // sequence that holds row m (-1: none): the last i with q_start[i] <= m, 64
 // candidates at a time
 __device__ __forceinline__ int seq_of_row(const AttnPages& a, int m) {
@@ -454,29 +825,36 @@ __device__ __forceinline__ int seq_of_row(const AttnPages& a, int m) {
 
 // Adds the splits of a row's head: threads on four dimensions each take the
 // splits by turns, all their loads at once, and the groups of threads are added
-// in order.
-template <int D>
-__global__ __launch_bounds__(256) void attn_pages_merge_k(AttnPages a) {
-  constexpr int LANES = D / 4, GROUPS = 256 / LANES, EACH = (kMaxSplits + GROUPS - 1) / GROUPS;
-  const int m = blockIdx.x, h = blockIdx.y;
-  const int i = seq_of_row(a, m);
-  if (i < 0) return;
+// in order.  Up to kSmallMerge splits a wave does it alone, four heads to a
+// workgroup (2036 rows of 32 heads in two parts: 58 -> 11 us); above, a workgroup.
+// Sequences of few columns by (sequence, row of up to few_rows), the others by row.
+constexpr int kSmallMerge = 8;
+template <int D, int MAX, bool FEW>
+__global__ __launch_bounds__(256) void attn_pages_merge_k(AttnPages a, int few_rows) {
+  constexpr bool WAVE = MAX <= kSmallMerge;
+  constexpr int LANES = D / 4, GROUPS = (WAVE ? 64 : 256) / LANES, EACH = (MAX + GROUPS - 1) / GROUPS;
+  const int h = WAVE ? 4 * blockIdx.y + (threadIdx.x >> 6) : blockIdx.y;
+  const int i = FEW ? blockIdx.x / few_rows : seq_of_row(a, blockIdx.x);
+  if (i < 0 || h >= a.H) return;
   const Seq s = sequence(a, i);
-  const int ns = max(1, (s.len + a.chunk - 1) / a.chunk);
-  if (ns == 1 || m - s.row0 >= a.max_q) return;
+  const int j = FEW ? blockIdx.x - i * few_rows : blockIdx.x - s.row0, m = s.row0 + j;
+  const int chunk = FEW ? a.chunk_few : a.chunk_many;
+  const int ns = max(1, (s.len + chunk - 1) / chunk);
+  if (ns == 1 || j >= min(s.nq, a.max_q) || FEW != (s.nq * a.G <= kFewCols)) return;
   const int64_t at = ((int64_t)m * a.H + h) * a.splits;
-  const int tid = threadIdx.x, lane = tid & 63, grp = tid / LANES, dim = 4 * (tid % LANES);
+  const int lane = threadIdx.x & 63, t = WAVE ? lane : threadIdx.x;
+  const int grp = t / LANES, dim = 4 * (t % LANES);
   f4 x[EACH];
 #pragma unroll
   for (int j = 0; j < EACH; ++j)
     if (grp + j * GROUPS < ns)
       x[j] = *reinterpret_cast<const f4*>(a.part + (at + grp + j * GROUPS) * D + dim);
   const float2 rl = lane < ns ? a.part_rl[at + lane] : make_float2(-INFINITY, 0.f);
-  float R = rl.x, w = 0.f, L = 0.f;
+  float R = rl.x, w = 0.f;
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) R = fmaxf(R, wave_shfl_xor(R, d));
   if (R != -INFINITY) w = __builtin_amdgcn_exp2f(rl.x - R);
-  L = rl.y * w;
+  float L = rl.y * w;
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) L += wave_shfl_xor(L, d);
   f4 A = f4{0.f, 0.f, 0.f, 0.f};
@@ -487,26 +865,83 @@ __global__ __launch_bounds__(256) void attn_pages_merge_k(AttnPages a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) A[e] = __builtin_fmaf(x[j][e], f, A[e]);
   }
-  __shared__ f4 sum[GROUPS][LANES];
-  sum[grp][tid % LANES] = A;
-  __syncthreads();
-  if (tid >= D) return;
-  float v = 0.f;
-  for (int k = 0; k < GROUPS; ++k) v += sum[k][tid / 4][tid % 4];
-  a.o[(int64_t)m * a.ldo + (int64_t)h * D + tid] = f2h(L > 0.f ? v / L : (L == L ? 0.f : L));
+  const auto result = [&](float v) { return f2h(L > 0.f ? v / L : (L == L ? 0.f : L)); };
+  uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D;
+  if constexpr (WAVE) {
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float y = A[e];
+        A[e] = y + wave_shfl_xor(y, d);
+      }
+    if (grp > 0) return;
+    if (a.o_vec) {
+      *reinterpret_cast<u32x2*>(o + dim) =
+          u32x2{(uint32_t)result(A[0]) | ((uint32_t)result(A[1]) << 16),
+                (uint32_t)result(A[2]) | ((uint32_t)result(A[3]) << 16)};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[dim + e] = result(A[e]);
+    }
+  } else {
+    __shared__ f4 sum[GROUPS][LANES];
+    sum[grp][t % LANES] = A;
+    __syncthreads();
+    if (t >= D) return;
+    float v = 0.f;
+    for (int k = 0; k < GROUPS; ++k) v += sum[k][t / 4][t % 4];
+    o[t] = result(v);
+  }
 }
 
-// Splits: workgroups for the whole chip where the sequences' columns alone are
-// too few, at least 256 keys each.
-constexpr int kWantWGs = 1024, kMinChunk = 256;
+static int64_t col_tiles(int64_t max_q, int G, int tile) { return (max_q * G + tile - 1) / tile; }
 
-static int64_t col_tiles(int64_t max_q, int G) { return (max_q * G + 15) / 16; }
+// keys of each of S parts, in whole multiples of `round`
+static int chunk_of(int64_t max_len, int64_t S, int round) {
+  S = std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
+  return (int)std::max<int64_t>(round, ((max_len + S - 1) / S + round - 1) / round * round);
+}
 
-static int split_chunk(const pipo_kv_pages* c, int n_heads, int64_t max_q, int64_t max_len) {
-  const int64_t wgs = (int64_t)c->n_seq * c->n_kv_heads * col_tiles(max_q, n_heads / c->n_kv_heads);
-  int64_t S = std::min<int64_t>((kWantWGs + wgs - 1) / wgs, kMaxSplits);
-  S = std::max<int64_t>(1, std::min(S, max_len / kMinChunk));
-  return (int)(((max_len + S - 1) / S + 127) / 128 * 128);
+// Workgroups.  Few columns: four waves where that gives two workgroups a CU,
+// else eight, whose sums meet in LDS, and below one a CU the keys are split as
+// well, 256 at least each and from 768 on (a second kernel costs what 500 keys of
+// a workgroup do).  us, 32/8 heads, four waves against eight: 64 sequences of
+// 544 keys 16.1 against 20.4, 28 of 2100 26.6 against 22.5; 16 of 500 unsplit
+// 9.4, in two 11.0; 4 of 2000 20.1 and in eight 10.7; 1 of 8000 61.7 and in 32
+// 11.0.  Many columns: parts of 512 keys at least where there is not a
+// workgroup for each place on the chip, two a CU (509 rows over 4099 keys: one
+// sequence in two parts 125, in four 91; two in one 229, in two 153).
+constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
+
+struct Plan {
+  bool few, many;  // sequences that may be of either kind
+  bool wide;       // eight waves for those of few columns
+  int chunk_few, chunk_many, splits;
+};
+static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t max_q,
+                      int64_t max_len) {
+  const int G = n_heads / c->n_kv_heads;
+  Plan p;
+  p.many = max_q * G > kFewCols;
+  p.few = !p.many || G <= kFewCols;
+  const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, kFewCols / G));
+  // (with many columns about, most of the others have one row)
+  const int64_t wgs =
+      (int64_t)c->n_seq * c->n_kv_heads * (p.many ? col_tiles(1, G, 16) : col_tiles(few_q, G, 16));
+  p.wide = wgs < 2 * kCUs;
+  p.chunk_few = chunk_of(max_len, max_len < kSplitFew ? 1 : std::min(kCUs / wgs, max_len / kMinFew),
+                         kBlockKeys);
+  // (of all sequences, M rows in all)
+  const int64_t tiles = std::min<int64_t>(c->n_seq * col_tiles(max_q, G, kManyCols),
+                                          M * G / kManyCols + c->n_seq) * c->n_kv_heads;
+  p.chunk_many = chunk_of(max_len, std::min((2 * kCUs + tiles - 1) / tiles, max_len / kMinMany),
+                          kManyKeys);
+  if (M >= (1 << 23)) p.chunk_many = chunk_of(max_len, 1, kManyKeys);  // (a grid of M workgroups)
+  int chunk = p.chunk_few;
+  if (p.many) chunk = p.few ? std::min(chunk, p.chunk_many) : p.chunk_many;
+  p.splits = (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk);
+  return p;
 }
 
 static int64_t partial_bytes(int64_t M, int n_heads, int head_dim, int64_t splits) {
@@ -522,8 +957,10 @@ static pipo_status check_attn(const char* what, const pipo_kv_pages* c, int32_t 
               (long long)(c->table_stride * c->page_size));
     return PIPO_ERR_ARG;
   }
-  if (M * n_heads >= ((int64_t)1 << 31) || (int64_t)max_q * n_heads >= ((int64_t)1 << 31) ||
-      n_heads > 65535 || c->n_seq > 65535 || max_len > (1 << 30)) {
+  const int64_t cols = std::min<int64_t>(max_q, M) * (n_heads / c->n_kv_heads);
+  if (M * n_heads >= ((int64_t)1 << 31) || n_heads > 65535 || c->n_seq > 65535 ||
+      (int64_t)c->n_seq * c->n_kv_heads >= ((int64_t)1 << 22) || max_len > (1 << 30) ||
+      (cols + kManyCols - 1) / kManyCols * c->n_kv_heads >= ((int64_t)1 << 22)) {
     set_error("%s: %lld rows of %d heads, %d sequences of %d keys", what, (long long)M, n_heads,
               c->n_seq, max_len);
     return PIPO_ERR_UNSUPPORTED;
@@ -532,12 +969,43 @@ static pipo_status check_attn(const char* what, const pipo_kv_pages* c, int32_t 
 }
 
 template <int D>
-static void launch_attn_pages(const AttnPages& a, hipStream_t st) {
-  const dim3 grid((unsigned)(a.c.Hkv * col_tiles(a.max_q, a.G)), (unsigned)a.splits,
-                  (unsigned)a.c.n_seq);
-  launch(attn_pages_k<D, 4>, grid, dim3(256), 0, st, a);
-  if (a.splits > 1)
-    launch(attn_pages_merge_k<D>, dim3((unsigned)a.M, (unsigned)a.H), dim3(256), 0, st, a);
+static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st) {
+  const auto splits = [&](int chunk) {
+    return (unsigned)std::max(1, (a.max_len + chunk - 1) / chunk);
+  };
+  if (p.few) {
+    // Sequences fastest, so that workgroups with nothing to do (columns and
+    // splits that shorter ones lack) come in a row: workgroups go to the shader
+    // engines by turns, and with the column tiles of a sequence side by side those
+    // with work all went to one engine in four (28 sequences of 2100 keys among
+    // up to 16 rows: 63.8 us, 23 without)
+    const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, kFewCols);
+    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), splits(a.chunk_few), (unsigned)((cols + 15) / 16));
+    if (p.wide)
+      launch(attn_pages_few_k<D, 8>, g, dim3(512), 0, st, a);
+    else
+      launch(attn_pages_few_k<D, 4>, g, dim3(256), 0, st, a);
+  }
+  if (p.many)  // (an odd number of tiles: a sequence's first is on another engine each time)
+    launch(attn_pages_many_k<D>,
+           dim3((unsigned)(a.c.Hkv * (col_tiles(a.max_q, a.G, kManyCols) | 1)), splits(a.chunk_many),
+                (unsigned)a.c.n_seq),
+           dim3(256), 0, st, a);
+  const auto merge = [&](auto few_c, int chunk, int64_t rows, int few_rows) {
+    constexpr bool FEW = decltype(few_c)::value;
+    const unsigned n = splits(chunk);
+    if (n > kSmallMerge)
+      launch(attn_pages_merge_k<D, kMaxSplits, FEW>, dim3((unsigned)rows, (unsigned)a.H), dim3(256), 0,
+             st, a, few_rows);
+    else if (n > 1)
+      launch(attn_pages_merge_k<D, kSmallMerge, FEW>, dim3((unsigned)rows, (unsigned)((a.H + 3) / 4)),
+             dim3(256), 0, st, a, few_rows);
+  };
+  if (p.few) {
+    const int few_rows = std::max(1, std::min(a.max_q, kFewCols / a.G));
+    merge(std::true_type{}, a.chunk_few, (int64_t)a.c.n_seq * few_rows, few_rows);
+  }
+  if (p.many) merge(std::false_type{}, a.chunk_many, a.M, 0);
 }
 
 }  // namespace pipo
@@ -552,8 +1020,8 @@ int64_t pipo_op_attn_pages_workspace_bytes(const pipo_kv_pages* c, int32_t n_hea
       max_q < 1 || max_len < 1 || M < 1 ||
       check_attn("attn_pages", c, n_heads, M, max_q, max_len) != PIPO_OK)
     return 0;
-  const int chunk = split_chunk(c, n_heads, std::min<int64_t>(max_q, M), max_len);
-  return partial_bytes(M, n_heads, c->head_dim, (max_len + chunk - 1) / chunk);
+  return partial_bytes(M, n_heads, c->head_dim,
+                       plan_attn(c, n_heads, M, std::min<int64_t>(max_q, M), max_len).splits);
 }
 
 pipo_status pipo_op_attn_pages(const pipo_kv_pages* c, int32_t layer, const uint16_t* q, int64_t ldq,
@@ -584,19 +1052,20 @@ pipo_status pipo_op_attn_pages(const pipo_kv_pages* c, int32_t layer, const uint
   a.G = n_heads / c->n_kv_heads;
   a.max_q = (int)std::min<int64_t>(max_q, M);
   a.max_len = max_len;
-  a.chunk = split_chunk(c, n_heads, a.max_q, max_len);
-  a.splits = std::max(1, (max_len + a.chunk - 1) / a.chunk);
+  Plan p = plan_attn(c, n_heads, M, a.max_q, max_len);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 ||
-      workspace_bytes < partial_bytes(M, n_heads, c->head_dim, a.splits)) {
-    a.chunk = (max_len + 127) / 128 * 128;
-    a.splits = 1;
+      workspace_bytes < partial_bytes(M, n_heads, c->head_dim, p.splits)) {
+    p.chunk_few = p.chunk_many = std::max(128, (max_len + 127) / 128 * 128);
+    p.splits = 1;
   }
-  a.chunk = std::max(a.chunk, 128);
+  a.chunk_few = p.chunk_few;
+  a.chunk_many = p.chunk_many;
+  a.splits = p.splits;
   a.part_rl = reinterpret_cast<float2*>(a.part + M * n_heads * a.splits * c->head_dim);
   a.q_vec = reinterpret_cast<uintptr_t>(q) % 16 == 0 && ldq % 8 == 0;
   a.o_vec = reinterpret_cast<uintptr_t>(o) % 8 == 0 && ldo % 4 == 0;
   const auto go = c->head_dim == 128 ? launch_attn_pages<128> : launch_attn_pages<64>;
-  go(a, static_cast<hipStream_t>(stream));
+  go(a, p, static_cast<hipStream_t>(stream));
   PIPO_HIP_TRY(hipGetLastError());
   return PIPO_OK;
 }

@@ -76,7 +76,8 @@ def test_bad_rows(kw, want):
     (dict(n_heads=33), "PIPO_ERR_ARG"), (dict(n_heads=0), "PIPO_ERR_ARG"), (dict(M=-1), "PIPO_ERR_ARG"),
     (dict(max_q=-1), "PIPO_ERR_ARG"), (dict(max_len=513), "PIPO_ERR_ARG"),
     (dict(max_len=-1), "PIPO_ERR_ARG"), (dict(wsb=-1), "PIPO_ERR_ARG"),
-    (dict(M=1 << 26), "PIPO_ERR_UNSUPPORTED"), (dict(max_q=1 << 26), "PIPO_ERR_UNSUPPORTED"),
+    (dict(M=1 << 26), "PIPO_ERR_UNSUPPORTED"),
+    (dict(M=1 << 25, max_q=1 << 25), "PIPO_ERR_UNSUPPORTED"),
     (dict(n_heads=65536, ldq=1 << 24, ldo=1 << 24), "PIPO_ERR_UNSUPPORTED")])
 def test_bad_attention(kw, want):
     a = dict(q=P, ldq=4096, q_start=P, kv_len=P, o=P, ldo=4096, n_heads=32, M=4, max_q=1, max_len=512,

@@ -456,8 +456,9 @@ attn_pages_few_k(AttnPages a) {
   }
 }
 
-// Many columns: a workgroup is four waves of 32 columns each on (sequence,
-// key/value head, 128 columns, split).  They take the split's keys 64 at a time:
+// Many columns: a workgroup is one or two teams of four waves of 32 columns each
+// on (sequence, key/value head, 128 columns, split).  Two teams take the split's
+// keys by turns, 64 at a time, and meet in LDS at the end.  In a team
 // each wave unpacks a tile of the next block into LDS, in operand order (keys as c,
 // values as c - 7.5), while all of them work on this one, so a block is unpacked once for 128
 // columns and every LDS access is a wave's contiguous kilobyte.  The weights p s
@@ -511,8 +512,8 @@ __device__ __forceinline__ void as_halves(uint32_t (&w)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i]));
 }
 
-template <int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void
+template <int D, int TEAMS>
+__global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void
 attn_pages_many_k(AttnPages a) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16, T = kManyKeys / 16, U = 2;
   const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y, si = seq_in_order(a, blockIdx.z);
@@ -525,7 +526,8 @@ attn_pages_many_k(AttnPages a) {
   const int ns = max(1, (s.len + a.chunk_many - 1) / a.chunk_many);
   if (sp >= ns) return;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
+  const int team = __builtin_amdgcn_readfirstlane(tid >> 8);
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
 
@@ -538,13 +540,22 @@ attn_pages_many_k(AttnPages a) {
     uint32_t pair[2][T][16 * NG];
     uint32_t top[T], valid[T];
   };
-  __shared__ Stage st[2];
+  constexpr int ROW = D + 4;  // floats of a column's sums, where the teams meet
+  union Lds {
+    Stage st[TEAMS][2];
+    float sums[TEAMS - 1 ? kManyCols : 1][ROW];
+  };
+  __shared__ Lds lds;
+  __shared__ float2 lds_rl[TEAMS - 1 ? kManyCols : 1];
+  Stage* const st = lds.st[team];
 
   const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
   const int q_last = min(s.nq - 1, (kManyCols * ct + kManyCols - 1) / a.G);
   const int end = max(0, s.len - s.nq + q_last + 1);  // keys visible to any column
   const int p0 = sp * a.chunk_many, p1 = min(end, p0 + a.chunk_many);
   const int blocks = p1 > p0 ? (p1 - p0 + kManyKeys - 1) / kManyKeys : 0;
+  // this team's are blocks team, team + TEAMS .., and all waves go through as many
+  const int turns = (blocks + TEAMS - 1) / TEAMS, mine = (blocks + TEAMS - 1 - team) / TEAMS;
   // keys visible to all of the wave's columns, and to any
   const int all = max(0, s.len - s.nq + c0 / a.G + 1);
   const int end_w = c0 < cols ? min(p1, s.len - s.nq + min(s.nq - 1, (c0 + 31) / a.G) + 1) : 0;
@@ -554,13 +565,13 @@ attn_pages_many_k(AttnPages a) {
   u32x4 pw;
   uint32_t ok;
   int lim;
-  // lane i holds the page of its tile in block i, 64 blocks at a time
+  // lane i holds the page of its tile in the team's block i, 64 at a time
   const int32_t* row = a.c.table + si * a.c.stride;
   int pages = -1;
   const auto fetch = [&](int blk) {
-    const int pos = p0 + blk * kManyKeys + 16 * wave;
+    const int pos = p0 + (TEAMS * blk + team) * kManyKeys + 16 * wave;
     if ((blk & 63) == 0) {
-      const int64_t at = (int64_t)pos + (int64_t)lane * kManyKeys;
+      const int64_t at = (int64_t)pos + (int64_t)lane * (TEAMS * kManyKeys);
       pages = at < p1 ? row[at >> a.c.ps_log2] : -1;
     }
     lim = p1 - pos;
@@ -660,8 +671,7 @@ attn_pages_many_k(AttnPages a) {
           float v = 0.f;
 #pragma unroll
           for (int n = 0; n < NG; ++n) {
-            v = n == 0 ? lo_half(w[e * NG]) * qsum[u][0]
-                       : __builtin_fmaf(lo_half(w[e * NG + n]), qsum[u][n], v);
+            v = __builtin_fmaf(lo_half(w[e * NG + n]), qsum[u][n], v);
             v = __builtin_fmaf(hi_half(w[e * NG + n]), d[u][n][e], v);
           }
           if constexpr (EDGE) v = x.valid[j] && k0 + 16 * j + 4 * g + e < vis[u] ? v : -INFINITY;
@@ -739,7 +749,7 @@ attn_pages_many_k(AttnPages a) {
     }
   };
 
-  if (blocks > 0) {
+  if (mine > 0) {
     fetch(0);
     unpack(st[0]);
   }
@@ -749,32 +759,66 @@ attn_pages_many_k(AttnPages a) {
   // tile that is no page's; every wave goes through every block
   const auto run = [&](auto edge_c) {
     constexpr bool EDGE = decltype(edge_c)::value;
-    for (; blk < blocks; ++blk) {
+    for (; blk < turns; ++blk) {
       const Stage& x = st[blk & 1];
-      const int k0 = p0 + blk * kManyKeys;
+      const int k0 = p0 + (TEAMS * blk + team) * kManyKeys;
       if constexpr (!EDGE) {
         uint32_t v = 1;
 #pragma unroll
         for (int j = 0; j < T; ++j) v &= x.valid[j];
-        if (k0 + kManyKeys > all || !__builtin_amdgcn_readfirstlane(v)) return;
+        if (blk >= mine || k0 + kManyKeys > all || !__builtin_amdgcn_readfirstlane(v)) return;
       }
-      if (blk + 1 < blocks) fetch(blk + 1);
-      if (!EDGE || k0 < end_w) compute(x, k0, edge_c);
-      if (blk + 1 < blocks) unpack(st[(blk + 1) & 1]);
+      if (blk + 1 < mine) fetch(blk + 1);
+      if (!EDGE || (blk < mine && k0 < end_w)) compute(x, k0, edge_c);
+      if (blk + 1 < mine) unpack(st[(blk + 1) & 1]);
       __syncthreads();
     }
   };
   run(std::false_type{});
   run(std::true_type{});
 
-  // element e of acc[u][n]: dimension 16 n + 4 g + e of column c0 + 16 u + r
+  // element e of acc[u][n]: dimension 16 n + 4 g + e of column c0 + 16 u + r.  The
+  // second team's sums go to LDS (every block there is read), the first adds them.
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    l[u] = cols_sum(l[u]);
+#pragma unroll
+    for (int n = 0; n < NG; ++n) msum[u][n] = cols_sum(msum[u][n]);
+#pragma unroll
+    for (int n = 0; n < NF; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[u][n][e] += msum[u][n / 4];
+    const int c = 32 * wave + 16 * u + r;
+    if (team == 1) {
+#pragma unroll
+      for (int n = 0; n < NF; ++n)
+        *reinterpret_cast<f4*>(&lds.sums[c][16 * n + 4 * g]) = acc[u][n];
+      if (g == 0) lds_rl[c] = make_float2(R[u], l[u]);
+    }
+  }
+  if constexpr (TEAMS == 2) {
+    __syncthreads();
+    if (team == 1) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 32 * wave + 16 * u + r;
+      const float2 rl = lds_rl[c];
+      const float Rn = fmaxf(R[u], rl.x), Rs = Rn == -INFINITY ? 0.f : Rn;
+      const float f0 = __builtin_amdgcn_exp2f(R[u] - Rs), f1 = __builtin_amdgcn_exp2f(rl.x - Rs);
+      R[u] = Rn;
+      l[u] = l[u] * f0 + rl.y * f1;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        const f4 y = *reinterpret_cast<const f4*>(&lds.sums[c][16 * n + 4 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[u][n][e] = acc[u][n][e] * f0 + y[e] * f1;
+      }
+    }
+  }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int col = c0 + 16 * u + r;
-    const float L = cols_sum(l[u]);
-    float ms[NG];
-#pragma unroll
-    for (int n = 0; n < NG; ++n) ms[n] = cols_sum(msum[u][n]);
+    const float L = l[u];
     if (col >= cols) continue;
     const int m = s.row0 + col / a.G, h = kh * a.G + col % a.G;
     if (ns == 1) {
@@ -784,7 +828,7 @@ attn_pages_many_k(AttnPages a) {
       for (int n = 0; n < NF; ++n) {
         uint16_t v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = f2h((acc[u][n][e] + ms[n / 4]) * inv);
+        for (int e = 0; e < 4; ++e) v[e] = f2h(acc[u][n][e] * inv);
         if (a.o_vec) {
           *reinterpret_cast<u32x2*>(o + 16 * n + 4 * g) =
               u32x2{(uint32_t)v[0] | ((uint32_t)v[1] << 16), (uint32_t)v[2] | ((uint32_t)v[3] << 16)};
@@ -797,10 +841,7 @@ attn_pages_many_k(AttnPages a) {
       const int64_t at = ((int64_t)m * a.H + h) * a.splits + sp;
 #pragma unroll
       for (int n = 0; n < NF; ++n) {
-        f4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[u][n][e] + ms[n / 4];
-        *reinterpret_cast<f4*>(a.part + at * D + 16 * n + 4 * g) = v;
+        *reinterpret_cast<f4*>(a.part + at * D + 16 * n + 4 * g) = acc[u][n];
       }
       if (g == 0) a.part_rl[at] = make_float2(R[u], L);
     }
@@ -909,14 +950,17 @@ static int chunk_of(int64_t max_len, int64_t S, int round) {
 // a workgroup do).  us, 32/8 heads, four waves against eight: 64 sequences of
 // 544 keys 16.1 against 20.4, 28 of 2100 26.6 against 22.5; 16 of 500 unsplit
 // 9.4, in two 11.0; 4 of 2000 20.1 and in eight 10.7; 1 of 8000 61.7 and in 32
-// 11.0.  Many columns: parts of 512 keys at least where there is not a
-// workgroup for each place on the chip, two a CU (509 rows over 4099 keys: one
-// sequence in two parts 125, in four 91; two in one 229, in two 153).
+// 11.0.  Many columns: two teams, one workgroup a CU, up to three workgroups for
+// each, so that all SIMDs have two waves until the CU's last key; one team, two
+// workgroups a CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135
+// us against 155, eight 504 against 466; four over 509 to 4099 keys 150 against
+// 184).  Parts of 512 keys at least where there is not a workgroup for each CU.
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
 
 struct Plan {
   bool few, many;  // sequences that may be of either kind
   bool wide;       // eight waves for those of few columns
+  int teams;       // of a workgroup for the others
   int chunk_few, chunk_many, splits;
 };
 static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t max_q,
@@ -935,9 +979,10 @@ static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t ma
   // (of all sequences, M rows in all)
   const int64_t tiles = std::min<int64_t>(c->n_seq * col_tiles(max_q, G, kManyCols),
                                           M * G / kManyCols + c->n_seq) * c->n_kv_heads;
-  p.chunk_many = chunk_of(max_len, std::min((2 * kCUs + tiles - 1) / tiles, max_len / kMinMany),
+  p.chunk_many = chunk_of(max_len, std::min((kCUs + tiles - 1) / tiles, max_len / kMinMany),
                           kManyKeys);
   if (M >= (1 << 23)) p.chunk_many = chunk_of(max_len, 1, kManyKeys);  // (a grid of M workgroups)
+  p.teams = tiles > 3 * kCUs ? 1 : 2;
   int chunk = p.chunk_few;
   if (p.many) chunk = p.few ? std::min(chunk, p.chunk_many) : p.chunk_many;
   p.splits = (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk);
@@ -986,11 +1031,14 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
     else
       launch(attn_pages_few_k<D, 4>, g, dim3(256), 0, st, a);
   }
-  if (p.many)  // (an odd number of tiles: a sequence's first is on another engine each time)
-    launch(attn_pages_many_k<D>,
-           dim3((unsigned)(a.c.Hkv * (col_tiles(a.max_q, a.G, kManyCols) | 1)), splits(a.chunk_many),
-                (unsigned)a.c.n_seq),
-           dim3(256), 0, st, a);
+  if (p.many) {  // (an odd number of tiles: a sequence's first is on another engine each time)
+    const dim3 g((unsigned)(a.c.Hkv * (col_tiles(a.max_q, a.G, kManyCols) | 1)),
+                 splits(a.chunk_many), (unsigned)a.c.n_seq);
+    if (p.teams == 2)
+      launch(attn_pages_many_k<D, 2>, g, dim3(512), 0, st, a);
+    else
+      launch(attn_pages_many_k<D, 1>, g, dim3(256), 0, st, a);
+  }
   const auto merge = [&](auto few_c, int chunk, int64_t rows, int few_rows) {
     constexpr bool FEW = decltype(few_c)::value;
     const unsigned n = splits(chunk);

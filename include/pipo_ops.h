@@ -294,8 +294,9 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  *
  * M: rows of q and o; max_q, max_len: bounds of a sequence's rows and keys that
  * the host knows (max_len at most table_stride * page_size).  A length above
- * max_len counts as max_len, a start outside [0, M] as the nearer end, and rows
- * of a sequence with more than max_q of them may be left unwritten.  Keys on
+ * max_len counts as max_len, a start outside [0, M] as the nearer end, and of a
+ * sequence of more than max_q rows those past the max_q-th are left as they were.
+ * Keys on
  * an entry of the table that is not a page are not seen, a row that sees no
  * key becomes 0, rows outside q_start[0] .. q_start[n_seq] - 1 are left as
  * they were.

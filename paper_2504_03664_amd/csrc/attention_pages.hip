@@ -28,13 +28,15 @@ struct AttnPages {
   float2* part_rl;
   int64_t ldq, ldo, M;
   int H, G, max_q, max_len;
+  int few_cols;               // up to this many are attn_pages_few_k's, or none
   int chunk_few, chunk_many;  // keys of a split, by the sequence's columns
   int splits;                 // of a row's partials in `part`
   bool q_vec, o_vec;          // q rows 16-byte aligned, o rows 8-byte
 };
 
 // Up to this many columns a sequence is attn_pages_few_k's, above it
-// attn_pages_many_k's.
+// attn_pages_many_k's; all of them where every row of the call may be one of
+// max_q equal shares, which saves a launch.
 constexpr int kFewCols = 64;
 constexpr int kBlockKeys = 32;  // of attn_pages_few_k
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
@@ -42,9 +44,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^15 / (a bound of the values' scales), so that p s fits a half
 constexpr float kPBits = 15.f;
 
-// a sequence's rows [row0, row0 + nq) and keys
+// a sequence's rows [row0, row0 + nq), how many of them count (up to max_q), and
+// keys
 struct Seq {
-  int row0, nq, len;
+  int row0, nq, rows, len;
 };
 __device__ __forceinline__ Seq sequence(const AttnPages& a, int i) {
   Seq s;
@@ -52,6 +55,7 @@ __device__ __forceinline__ Seq sequence(const AttnPages& a, int i) {
   const int64_t r1 = min(max((int64_t)a.q_start[i + 1], r0), a.M);
   s.row0 = (int)r0;
   s.nq = (int)(r1 - r0);
+  s.rows = min(s.nq, a.max_q);
   s.len = min(max(a.kv_len[i], 0), a.max_len);
   return s;
 }
@@ -224,8 +228,8 @@ attn_pages_few_k(AttnPages a) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16;
   const int kh = blockIdx.x % a.c.Hkv, si = blockIdx.x / a.c.Hkv, sp = blockIdx.y, ct = blockIdx.z;
   const Seq s = sequence(a, si);
-  const int cols = s.nq * a.G;
-  if (16 * ct >= cols || cols > kFewCols) return;
+  const int cols = s.rows * a.G;
+  if (16 * ct >= cols || cols > a.few_cols) return;
   const int ns = max(1, (s.len + a.chunk_few - 1) / a.chunk_few);
   if (sp >= ns) return;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -243,7 +247,7 @@ attn_pages_few_k(AttnPages a) {
   // this lane's column: keys [0, vis) are visible
   const int col = 16 * ct + r, qj = col / a.G, h = kh * a.G + col % a.G;
   const int vis = col < cols ? max(0, s.len - s.nq + qj + 1) : 0;
-  const int jmin = 16 * ct / a.G, jmax = min(s.nq - 1, (16 * ct + 15) / a.G);
+  const int jmin = 16 * ct / a.G, jmax = min(s.rows - 1, (16 * ct + 15) / a.G);
   const int all = max(0, s.len - s.nq + jmin + 1);      // visible to every column
   const int end = max(0, s.len - s.nq + jmax + 1);      // to any
   const int p0 = sp * a.chunk_few, p1 = min(end, p0 + a.chunk_few);
@@ -484,18 +488,51 @@ __device__ __forceinline__ h4 v_centred(uint32_t w, const Magic& g) {
   return __builtin_bit_cast(h4, o) - h4{b, b, b, b};
 }
 
-// Sequence at place z of the launch: up to 64 sequences go by their keys, the most
-// first (16 prompts' 509 rows each over 509 to 4099 keys: 556 -> 489 us).
-__device__ __forceinline__ int seq_in_order(const AttnPages& a, int z) {
+// The t-th column tile of the launch: its sequence (-1: none) and which of the
+// sequence's tiles.  Only sequences of many columns have tiles, so that a batch of
+// which a few are prompts launches little else (a workgroup with nothing to do
+// waits for as much LDS as the others).  Up to 64 sequences go by their keys, the
+// most first (16 prompts' 509 rows each over 509 to 4099 keys: 556 -> 489 us).
+// Of a sequence the tiles with the most keys come first.
+struct Place {
+  int seq, tile;
+};
+__device__ __forceinline__ int many_tiles(const AttnPages& a, int i) {
+  const int cols = sequence(a, i).rows * a.G;
+  return cols > a.few_cols ? (cols + kManyCols - 1) / kManyCols : 0;
+}
+__device__ __forceinline__ Place place_of(const AttnPages& a, int t) {
   const int n = a.c.n_seq, lane = threadIdx.x & 63;
-  if (n == 1 || n > 64) return z;
-  const int keys = lane < n ? a.kv_len[lane] : 0;
-  int rank = 0;
-  for (int i = 0; i < n; ++i) {
-    const int k = __builtin_amdgcn_readlane(keys, i);
-    rank += k > keys || (k == keys && i < lane);
+  if (n <= 64) {
+    const int tiles = lane < n ? many_tiles(a, lane) : 0, keys = tiles ? a.kv_len[lane] : 0;
+    int before = 0;
+    for (int i = 0; i < n; ++i) {
+      const int k = __builtin_amdgcn_readlane(keys, i), w = __builtin_amdgcn_readlane(tiles, i);
+      before += k > keys || (k == keys && i < lane) ? w : 0;
+    }
+    const uint64_t hit = __ballot(t >= before && t < before + tiles);
+    if (!hit) return Place{-1, 0};
+    const int i = __ffsll((unsigned long long)hit) - 1;
+    return Place{i, __builtin_amdgcn_readlane(before + tiles - 1, i) - t};
   }
-  return __ffsll((unsigned long long)__ballot(lane < n && rank == z)) - 1;
+  const int each = (n + 63) / 64, first = lane * each, last = min(n, first + each);
+  int sum = 0;
+  for (int i = first; i < last; ++i) sum += many_tiles(a, i);
+  int end = sum;  // of this lane's tiles
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(end, d, 64);
+    if (lane >= d) end += y;
+  }
+  const uint64_t hit = __ballot(t >= end - sum && t < end);
+  if (!hit) return Place{-1, 0};
+  const int src = __ffsll((unsigned long long)hit) - 1;
+  int r = t - __builtin_amdgcn_readlane(end - sum, src);
+  for (int i = src * each;; ++i) {  // (ends: r is below the sum of these)
+    const int tiles = many_tiles(a, i);
+    if (r < tiles) return Place{i, tiles - 1 - r};
+    r -= tiles;
+  }
 }
 
 template <int CTRL>
@@ -516,13 +553,13 @@ template <int D, int TEAMS>
 __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void
 attn_pages_many_k(AttnPages a) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16, T = kManyKeys / 16, U = 2;
-  const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y, si = seq_in_order(a, blockIdx.z);
+  const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y;
+  const Place at = place_of(a, blockIdx.x / a.c.Hkv);
+  if (at.seq < 0) return;
+  const int si = __builtin_amdgcn_readfirstlane(at.seq);
+  const int ct = __builtin_amdgcn_readfirstlane(at.tile);
   const Seq s = sequence(a, si);
-  const int cols = s.nq * a.G;
-  if (cols <= kFewCols) return;
-  // the tiles with the most keys first
-  const int ct = (int)(gridDim.x / a.c.Hkv) - 1 - (int)(blockIdx.x / a.c.Hkv);
-  if (kManyCols * ct >= cols) return;
+  const int cols = s.rows * a.G;
   const int ns = max(1, (s.len + a.chunk_many - 1) / a.chunk_many);
   if (sp >= ns) return;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -550,7 +587,7 @@ attn_pages_many_k(AttnPages a) {
   Stage* const st = lds.st[team];
 
   const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
-  const int q_last = min(s.nq - 1, (kManyCols * ct + kManyCols - 1) / a.G);
+  const int q_last = min(s.rows - 1, (kManyCols * ct + kManyCols - 1) / a.G);
   const int end = max(0, s.len - s.nq + q_last + 1);  // keys visible to any column
   const int p0 = sp * a.chunk_many, p1 = min(end, p0 + a.chunk_many);
   const int blocks = p1 > p0 ? (p1 - p0 + kManyKeys - 1) / kManyKeys : 0;
@@ -558,7 +595,7 @@ attn_pages_many_k(AttnPages a) {
   const int turns = (blocks + TEAMS - 1) / TEAMS, mine = (blocks + TEAMS - 1 - team) / TEAMS;
   // keys visible to all of the wave's columns, and to any
   const int all = max(0, s.len - s.nq + c0 / a.G + 1);
-  const int end_w = c0 < cols ? min(p1, s.len - s.nq + min(s.nq - 1, (c0 + 31) / a.G) + 1) : 0;
+  const int end_w = c0 < cols ? min(p1, s.len - s.nq + min(s.rows - 1, (c0 + 31) / a.G) + 1) : 0;
 
   // this wave's tile of the next block, on its way
   uint32_t kw[KK], vw[KK];
@@ -881,7 +918,7 @@ __global__ __launch_bounds__(256) void attn_pages_merge_k(AttnPages a, int few_r
   const int j = FEW ? blockIdx.x - i * few_rows : blockIdx.x - s.row0, m = s.row0 + j;
   const int chunk = FEW ? a.chunk_few : a.chunk_many;
   const int ns = max(1, (s.len + chunk - 1) / chunk);
-  if (ns == 1 || j >= min(s.nq, a.max_q) || FEW != (s.nq * a.G <= kFewCols)) return;
+  if (ns == 1 || j >= s.rows || FEW != (s.rows * a.G <= a.few_cols)) return;
   const int64_t at = ((int64_t)m * a.H + h) * a.splits;
   const int lane = threadIdx.x & 63, t = WAVE ? lane : threadIdx.x;
   const int grp = t / LANES, dim = 4 * (t % LANES);
@@ -961,6 +998,7 @@ struct Plan {
   bool few, many;  // sequences that may be of either kind
   bool wide;       // eight waves for those of few columns
   int teams;       // of a workgroup for the others
+  int64_t tiles;   // of 128 columns they have at most
   int chunk_few, chunk_many, splits;
 };
 static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t max_q,
@@ -968,7 +1006,7 @@ static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t ma
   const int G = n_heads / c->n_kv_heads;
   Plan p;
   p.many = max_q * G > kFewCols;
-  p.few = !p.many || G <= kFewCols;
+  p.few = !p.many || (G <= kFewCols && M < c->n_seq * max_q);
   const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, kFewCols / G));
   // (with many columns about, most of the others have one row)
   const int64_t wgs =
@@ -976,9 +1014,11 @@ static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t ma
   p.wide = wgs < 2 * kCUs;
   p.chunk_few = chunk_of(max_len, max_len < kSplitFew ? 1 : std::min(kCUs / wgs, max_len / kMinFew),
                          kBlockKeys);
-  // (of all sequences, M rows in all)
-  const int64_t tiles = std::min<int64_t>(c->n_seq * col_tiles(max_q, G, kManyCols),
-                                          M * G / kManyCols + c->n_seq) * c->n_kv_heads;
+  p.tiles = std::min(c->n_seq * col_tiles(max_q, G, kManyCols), M * G / kManyCols + c->n_seq);
+  // (of n columns above 64, at most n / 64.5)
+  static_assert(kManyCols == 2 * kFewCols, "the bound of a sequence's tiles");
+  if (p.few) p.tiles = std::min(p.tiles, 2 * M * G / 129);
+  const int64_t tiles = std::max<int64_t>(1, p.tiles * c->n_kv_heads);
   p.chunk_many = chunk_of(max_len, std::min((kCUs + tiles - 1) / tiles, max_len / kMinMany),
                           kManyKeys);
   if (M >= (1 << 23)) p.chunk_many = chunk_of(max_len, 1, kManyKeys);  // (a grid of M workgroups)
@@ -1031,9 +1071,8 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
     else
       launch(attn_pages_few_k<D, 4>, g, dim3(256), 0, st, a);
   }
-  if (p.many) {  // (an odd number of tiles: a sequence's first is on another engine each time)
-    const dim3 g((unsigned)(a.c.Hkv * (col_tiles(a.max_q, a.G, kManyCols) | 1)),
-                 splits(a.chunk_many), (unsigned)a.c.n_seq);
+  if (p.many && p.tiles > 0) {
+    const dim3 g((unsigned)(a.c.Hkv * p.tiles), splits(a.chunk_many));
     if (p.teams == 2)
       launch(attn_pages_many_k<D, 2>, g, dim3(512), 0, st, a);
     else
@@ -1053,7 +1092,7 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
     const int few_rows = std::max(1, std::min(a.max_q, kFewCols / a.G));
     merge(std::true_type{}, a.chunk_few, (int64_t)a.c.n_seq * few_rows, few_rows);
   }
-  if (p.many) merge(std::false_type{}, a.chunk_many, a.M, 0);
+  if (p.many && p.tiles > 0) merge(std::false_type{}, a.chunk_many, a.M, 0);
 }
 
 }  // namespace pipo
@@ -1106,6 +1145,7 @@ pipo_status pipo_op_attn_pages(const pipo_kv_pages* c, int32_t layer, const uint
     p.chunk_few = p.chunk_many = std::max(128, (max_len + 127) / 128 * 128);
     p.splits = 1;
   }
+  a.few_cols = p.few ? kFewCols : 0;
   a.chunk_few = p.chunk_few;
   a.chunk_many = p.chunk_many;
   a.splits = p.splits;

@@ -302,6 +302,38 @@ def test_attention(lens, rows, H, Hkv, D, ps, shift, pad):
         assert err <= np.sqrt(2 / 3) * HALF * 1.1, err
 
 
+@pytest.mark.parametrize("n", [64, 65, 200])
+def test_attention_of_many_sequences(n):
+    """Prompts' pieces among single rows, over the counts at which workgroups find
+    their sequence in another way; columns at 64, 65, 128 and 129."""
+    print(f"attn sequences n={n}", flush=True)
+    rng = np.random.default_rng(n)
+    H, Hkv, D = 4, 2, 64
+    rows = [int(x) for x in rng.choice([0, 1, 1, 1, 2, 32, 33, 64, 65, 90], n)]
+    lens = [r + int(x) for r, x in zip(rows, rng.integers(0, 60, n))]
+    c = Cache(lens, Hkv, D, 16, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 1.5 * D ** -0.5).astype(np.float16)
+    got = attend(c, q, rows, H)
+    want, tol = want_attention(q, k, v, rows, lens, H, D)
+    check(got[:len(q)], want, tol, "many sequences")
+    assert (got[len(q):] == 9).all()
+
+
+def test_attention_of_equal_shares_that_are_not():
+    """As many rows as sequences times max_q, and sequences of fewer rows behind
+    which some belong to none."""
+    rng = np.random.default_rng(13)
+    H, Hkv, D, rows, lens = 8, 2, 128, [40, 1, 0, 12], [100, 300, 20, 12]
+    c = Cache(lens, Hkv, D, 32, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 0.1).astype(np.float16)
+    got = attend(c, q, rows, H, behind=4 * 40 - sum(rows))
+    want, tol = want_attention(q, k, v, rows, lens, H, D)
+    check(got[:len(q)], want, tol, "shares")
+    assert (got[len(q):] == 9).all()
+
+
 @pytest.mark.parametrize("lens,rows,H,Hkv,D,ps", [
     ([4000], [1], 8, 2, 128, 64), ([3001, 1, 0, 2600], [1, 1, 1, 1], 4, 4, 64, 16),
     ([2100, 5000], [3, 1], 8, 1, 128, 128), ([3000, 700], [100, 1], 4, 1, 128, 32),
@@ -361,6 +393,11 @@ def test_attention_with_wrong_lengths_starts_and_pages(rows):
         o = O.page_attention(q[at:at + r].reshape(r, H, D), k[i], v[i], seen).reshape(r, -1)
         check(got[at:at + r], o, HALF * np.abs(o) + 2 * HALF * np.abs(v[i]).max(), "pages")
         at += r
+    for most in (1, 17, 65):          # rows past the max_q-th of a sequence are left
+        got, at = attend(c, q, rows, H, max_q=most), 0
+        for r in rows:
+            assert (got[at + most:at + r] == 9).all() and (got[at:at + min(r, most)] != 9).any()
+            at += r
     total = sum(rows)
     for starts in ([-7, rows[0], total, 1 << 30], [0, 5, 3, total], [1 << 30] * 4):
         got = attend(c, q, rows, H, starts=starts, max_q=max(rows))

@@ -5,7 +5,10 @@
 //                   (kvquant.h) on elements clamped to +-kKvClamp (NaN: 0).
 //   pages_read_k:   slots -> fp16 rows, code * scale + min rounded once.
 //   pages_copy_k:   whole pages of every layer.
-// D/8 lanes hold one head's key (or value) of a row, eight elements each.
+// D/8 lanes hold one head's key (or value) of a row, eight elements each; the
+// lanes of one head in four rows follow each other, so that prompts, whose rows
+// are consecutive positions, write whole words of four keys' codes and 64 bytes
+// at a time.  Bound by HBM for prompts, by the launch for a decode step.
 #include "kvpages.h"
 
 #include <algorithm>
@@ -20,33 +23,40 @@ struct Slot {
   int64_t m;
   int head, x, key;   // x: eight-element piece
   bool value;
+  int seq, pos;
   const uint8_t* tile;
 };
 template <int D>
 __device__ __forceinline__ bool slot_of(const PagesView& c, const int32_t* seq, const int32_t* pos,
                                         int64_t M, Slot& s) {
   constexpr int LANES = D / 8;
-  const uint32_t per_row = (uint32_t)c.Hkv * 2 * LANES;
+  const uint32_t per_quad = (uint32_t)c.Hkv * 2 * 4 * LANES;  // of four rows
   const int64_t e = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-  if (e >= M * per_row) return false;
+  const int64_t quads = (M + 3) / 4;
+  if (e >= quads * per_quad) return false;
   uint32_t r;
-  if (M * per_row < ((int64_t)1 << 32)) {
-    const uint32_t row = (uint32_t)e / per_row;
-    s.m = row;
-    r = (uint32_t)e - row * per_row;
+  if (quads * per_quad < ((int64_t)1 << 32)) {
+    const uint32_t quad = (uint32_t)e / per_quad;
+    s.m = 4 * (int64_t)quad;
+    r = (uint32_t)e - quad * per_quad;
   } else {
-    s.m = e / per_row;
-    r = (uint32_t)(e - s.m * per_row);
+    s.m = e / per_quad;
+    r = (uint32_t)(e - s.m * per_quad);
+    s.m *= 4;
   }
-  // value heads behind key heads, as a fused projection's rows have them
   s.x = r % LANES;
-  s.head = r / LANES;
+  s.m += r / LANES % 4;
+  // value heads behind key heads, as a fused projection's rows have them
+  s.head = r / LANES / 4;
   s.value = s.head >= c.Hkv;
   if (s.value) s.head -= c.Hkv;
+  if (s.m >= M) return false;
   const int i = seq[s.m], p = pos[s.m];
   if (i < 0 || i >= c.n_seq || p < 0 || (p >> c.ps_log2) >= c.stride) return false;
   const int page = c.table[i * c.stride + (p >> c.ps_log2)];
   if (page < 0 || page >= c.n_pages) return false;
+  s.seq = i;
+  s.pos = p;
   s.key = p & (kTileKeys - 1);
   s.tile = tile_at<D>(c, page, s.head, p);
   return true;
@@ -58,8 +68,18 @@ __global__ __launch_bounds__(256) void pages_append_k(PagesView c, const int32_t
                                                       const uint16_t* __restrict__ k, int64_t ldk,
                                                       const uint16_t* __restrict__ v, int64_t ldv,
                                                       int64_t M) {
+  constexpr int LANES = D / 8;
   Slot s;
-  if (!slot_of<D>(c, seq, pos, M, s)) return;
+  const bool ok = slot_of<D>(c, seq, pos, M, s);
+  // whether the four rows of these 4 LANES lanes are the four keys of a word: each
+  // finds its own place counted from the first's
+  const int k4 = threadIdx.x / LANES % 4, first = (threadIdx.x & 63) - k4 * LANES;
+  const int at0 = ok ? s.pos - k4 : -1;
+  const uint64_t fit = __ballot(ok && at0 % 4 == 0 && at0 == __shfl(at0, first, 64) &&
+                                s.seq == __shfl(ok ? s.seq : -1, first, 64));
+  const uint64_t mask = LANES == 16 ? ~0ull : 0xFFFFFFFFull << (threadIdx.x & 32);
+  const bool whole = (fit & mask) == mask;
+  if (!ok) return;
   const uint16_t* src = (s.value ? v + s.m * ldv : k + s.m * ldk) + s.head * D + 8 * s.x;
   float f[8];
   if constexpr (VEC) {
@@ -90,10 +110,23 @@ __global__ __launch_bounds__(256) void pages_append_k(PagesView c, const int32_t
     const bool high = s.x & 2;
     const uint32_t lo = high ? o >> 16 : w, hi = high ? w >> 16 : o;
     uint8_t* at = tile + 8 * D + (8 * (s.x & 1) + (high ? 4 : 0) + 16 * (s.key >> 2)) * (D / 8) +
-                  4 * (s.x >> 2) + (s.key & 3);
+                  4 * (s.x >> 2);
+    uint32_t b = 0;  // byte j: of the j-th of the four
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      at[j * (D / 8)] = (uint8_t)(((lo >> (4 * j)) & 15) | (((hi >> (4 * j)) & 15) << 4));
+      b |= (((lo >> (4 * j)) & 15) | (((hi >> (4 * j)) & 15) << 4)) << (8 * j);
+    if (whole) {
+      // the four rows' bytes transposed: the lane of key k writes the word of the
+      // k-th, first by pairs of keys, then by halves
+      const uint32_t o1 = (uint32_t)__shfl_xor((int)b, LANES, 64);
+      b = k4 & 1 ? __builtin_amdgcn_perm(b, o1, 0x07030501u) : __builtin_amdgcn_perm(o1, b, 0x06020400u);
+      const uint32_t o2 = (uint32_t)__shfl_xor((int)b, 2 * LANES, 64);
+      b = k4 & 2 ? __builtin_amdgcn_perm(b, o2, 0x07060302u) : __builtin_amdgcn_perm(o2, b, 0x05040100u);
+      *reinterpret_cast<uint32_t*>(at + k4 * (D / 8)) = b;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j * (D / 8) + (s.key & 3)] = (uint8_t)(b >> (8 * j));
+    }
   }
   if (s.x % 8 == 0)
     *reinterpret_cast<uint32_t*>(tile + (s.value ? 17 : 16) * D + s.key * (D / 16) + s.x / 8 * 4) =
@@ -220,10 +253,10 @@ static pipo_status check_rows(const char* what, const pipo_kv_pages* c, const in
   return PIPO_OK;
 }
 
-// a thread per 8 elements, in rows of 2^22 blocks (a launch takes under 2^32
-// threads in a dimension)
+// a thread per 8 elements of four rows at a time, in rows of 2^22 blocks (a launch
+// takes under 2^32 threads in a dimension)
 static dim3 rows_grid(const PagesView& c, int D, int64_t M) {
-  const int64_t blocks = (M * c.Hkv * 2 * (D / 8) + 255) / 256, row = (int64_t)1 << 22;
+  const int64_t blocks = ((M + 3) / 4 * 4 * c.Hkv * 2 * (D / 8) + 255) / 256, row = (int64_t)1 << 22;
   return dim3((unsigned)std::min(blocks, row), (unsigned)((blocks + row - 1) / row));
 }
 

@@ -47,10 +47,14 @@ __global__ __launch_bounds__(256) void kv_quant_k(const uint16_t* __restrict__ x
   float v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
-  const Quant8 q = quantize8(v);
-  uint32_t word = 0;
+  float mn = v[0], mx = v[0];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) word |= q.c[j] << (4 * j);
+  for (int j = 1; j < 8; ++j) {
+    mn = fminf(mn, v[j]);
+    mx = fmaxf(mx, v[j]);
+  }
+  const Quant8 q = quantize8<false>(v, group_min8(mn), group_max8(mx));
+  const uint32_t word = pack8(q, [](int j) { return j; });
   uint8_t* row = out + r * (d / 2 + d / 16);
   *reinterpret_cast<uint32_t*>(row + 4 * c) = word;
   if (c % 8 == 0)

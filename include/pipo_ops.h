@@ -250,8 +250,8 @@ int64_t pipo_kv_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_d
  * ldk, n_kv_heads), so both may lie in the rows of a fused projection; q_out
  * may be q with ldqo = ldq (k_out likewise), other overlaps are not allowed.
  * A row whose position is negative or not below n_pos is left as it was
- * (padding).  head_dim 64 or 128, else PIPO_ERR_UNSUPPORTED.  cos_sin is
- * 4-byte aligned; rows on 16 bytes run fastest.
+ * (padding).  head_dim 64 or 128 and M below 2^31, else PIPO_ERR_UNSUPPORTED.
+ * Rows on 16 bytes run fastest.
  */
 pipo_status pipo_op_qk_norm_rope(const uint16_t* q, int64_t ldq, const uint16_t* k, int64_t ldk,
                                  const uint16_t* q_gamma, const uint16_t* k_gamma,
@@ -308,7 +308,7 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  * to rounding.  Calls sharing a workspace must not overlap in time.  The
  * order of all sums is fixed by the arguments of the call.
  * n_heads and n_seq up to 65535, n_seq * n_kv_heads below 2^22, max_len up to
- * 2^30, min(M, max_q) * n_heads up to 2^29 - 2^22 and M * n_heads below 2^31,
+ * 2^30, min(M, max_q) * n_heads up to 2^29 - 2^22 and M * n_heads below 2^30,
  * else PIPO_ERR_UNSUPPORTED.
  */
 pipo_status pipo_op_attn_pages(const pipo_kv_pages* cache, int32_t layer, const uint16_t* q,

@@ -41,7 +41,9 @@ constexpr int kFewCols = 64;
 constexpr int kBlockKeys = 32;  // of attn_pages_few_k
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
 constexpr float kLog2e = 1.4426950408889634f;
-// p is held times 2^15 / (a bound of the values' scales), so that p s fits a half
+// p is held times 2^15 / (a bound of the block's value scales), so that p s fits a
+// half with 29 bits of range below the largest (of a head of two groups the smaller
+// scale's have what is left of them: 11 where scales are 2^18 apart)
 constexpr float kPBits = 15.f;
 
 // a sequence's rows [row0, row0 + nq), how many of them count (up to max_q), and
@@ -1043,7 +1045,7 @@ static pipo_status check_attn(const char* what, const pipo_kv_pages* c, int32_t 
     return PIPO_ERR_ARG;
   }
   const int64_t cols = std::min<int64_t>(max_q, M) * (n_heads / c->n_kv_heads);
-  if (M * n_heads >= ((int64_t)1 << 31) || n_heads > 65535 || c->n_seq > 65535 ||
+  if (M * n_heads >= ((int64_t)1 << 30) || n_heads > 65535 || c->n_seq > 65535 ||
       (int64_t)c->n_seq * c->n_kv_heads >= ((int64_t)1 << 22) || max_len > (1 << 30) ||
       (cols + kManyCols - 1) / kManyCols * c->n_kv_heads >= ((int64_t)1 << 22)) {
     set_error("%s: %lld rows of %d heads, %d sequences of %d keys", what, (long long)M, n_heads,

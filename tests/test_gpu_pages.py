@@ -323,6 +323,39 @@ def test_attention_of_many_sequences(n):
     assert (got[len(q):] == 9).all()
 
 
+def test_attention_of_many_column_tiles():
+    """More column tiles than three a CU: one team a workgroup."""
+    rng = np.random.default_rng(14)
+    n, H, Hkv, D = 12, 64, 8, 64
+    rows = [130] * (n - 1) + [129]
+    lens = [r + int(x) for r, x in zip(rows, rng.integers(0, 90, n))]
+    c = Cache(lens, Hkv, D, 32, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 1.5 * D ** -0.5).astype(np.float16)
+    got = attend(c, q, rows, H)
+    want, tol = want_attention(q, k, v, rows, lens, H, D)
+    check(got[:len(q)], want, tol, "many tiles")
+
+
+@pytest.mark.parametrize("lens,rows,H,Hkv,split", [
+    ([9000], [1], 2, 1, False),              # eight waves
+    ([4500] + [1] * 511, [1] * 512, 2, 1, True),    # four waves
+    ([9000], [40], 4, 1, False), ([40000], [17], 8, 1, False), ([40000], [1], 2, 1, True)])
+def test_attention_past_a_waves_page_indices(lens, rows, H, Hkv, split):
+    """Waves hold the pages of 32 (64) of their blocks at a time."""
+    print(f"attn long lens={lens[:2]} rows={rows[:2]} split={split}", flush=True)
+    rng = np.random.default_rng(lens[0])
+    D = 64
+    c = Cache(lens, Hkv, D, 16, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 2 * D ** -0.5).astype(np.float16)
+    got = attend(c, q, rows, H, split=split)
+    want, tol = want_attention(q, k, v, rows, lens, H, D)
+    check(got[:len(q)], want, tol, "long")
+    err = np.linalg.norm(got[:len(q)].astype(np.float64) - want) / np.linalg.norm(want)
+    assert err <= np.sqrt(2 / 3) * HALF * 1.1, err
+
+
 def test_attention_of_equal_shares_that_are_not():
     """As many rows as sequences times max_q, and sequences of fewer rows behind
     which some belong to none."""

@@ -38,7 +38,7 @@ struct AttnPages {
 // attn_pages_many_k's; all of them where every row of the call may be one of
 // max_q equal shares, which saves a launch.
 constexpr int kFewCols = 64;
-constexpr int kBlockKeys = 32;  // of attn_pages_few_k
+constexpr int kPackCols = 8;  // columns with which 64 keys at a time can be taken
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^15 / (a bound of the block's value scales), so that p s fits a
@@ -208,6 +208,41 @@ __device__ __forceinline__ void read_part(Part<D>& t, uint32_t codes, uint32_t p
   }
 }
 
+// the codes of two tiles alone
+template <int D, int OFF>
+__device__ __forceinline__ void read_codes(uint32_t (&c)[2][D / 32], uint32_t codes) {
+  constexpr int T = kTileBytes<D>;
+  if constexpr (D == 128) {
+    u32x4 c0, c1;
+    asm volatile(
+        "ds_read_b128 %0, %2 offset:%3\n"
+        "ds_read_b128 %1, %2 offset:%4\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(c0), "=&v"(c1)
+        : "v"(codes), "n"(OFF), "n"(OFF + T)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      c[0][i] = c0[i];
+      c[1][i] = c1[i];
+    }
+  } else {
+    u32x2 c0, c1;
+    asm volatile(
+        "ds_read_b64 %0, %2 offset:%3\n"
+        "ds_read_b64 %1, %2 offset:%4\n"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(c0), "=&v"(c1)
+        : "v"(codes), "n"(OFF), "n"(OFF + T)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c[0][i] = c0[i];
+      c[1][i] = c1[i];
+    }
+  }
+}
+
 // result of column r of a tile of 16 columns: straight to o, or a partial
 template <int D>
 __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int row, int sp, int ns,
@@ -221,17 +256,22 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
   }
 }
 
-// Few columns: a workgroup is W waves on (sequence, key/value head, 16 columns,
-// split) that take the split's keys by turns, 32 at a time, from the cache into
-// operand registers.
-template <int D, int W>
-__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(3))) void
+// Few columns: a workgroup is W waves on (sequence, key/value head, 16 / PACK
+// columns, split) that take the split's keys by turns, 32 PACK at a time, through
+// LDS of their own: two blocks each, the next loaded while one is worked on.
+// PACK 2, for at most eight columns: the operands of a block's first 32 keys have
+// the queries in columns 0..7 and zeros in the others, those of its second 32 the
+// reverse, so the products of both meet in one register, and everything per score
+// is done once for 64 keys.
+template <int D, int W, int PACK>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(PACK == 2 ? 2 : 3))) void
 attn_pages_few_k(AttnPages a) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16;
+  constexpr int T = 2 * PACK, KEYS = 16 * T, COLS = 16 / PACK;  // tiles and keys of a block, columns
   const int kh = blockIdx.x % a.c.Hkv, si = blockIdx.x / a.c.Hkv, sp = blockIdx.y, ct = blockIdx.z;
   const Seq s = sequence(a, si);
   const int cols = s.rows * a.G;
-  if (16 * ct >= cols || cols > a.few_cols) return;
+  if (COLS * ct >= cols || cols > a.few_cols) return;
   const int ns = max(1, (s.len + a.chunk_few - 1) / a.chunk_few);
   if (sp >= ns) return;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -239,7 +279,7 @@ attn_pages_few_k(AttnPages a) {
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
   // two blocks a wave; the waves' sums at the end
-  constexpr int BLK = 2 * kTileBytes<D>, ROW = D + 4;
+  constexpr int BLK = T * kTileBytes<D>, ROW = D + 4;
   static_assert(16 * ROW * 4 <= 2 * BLK, "a wave's sums fit its blocks");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[W * 2 * BLK];
   __shared__ float lR[W][16], ll[W][16];
@@ -247,9 +287,10 @@ attn_pages_few_k(AttnPages a) {
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
 
   // this lane's column: keys [0, vis) are visible
-  const int col = 16 * ct + r, qj = col / a.G, h = kh * a.G + col % a.G;
+  // (PACK 2: of the first half block, or for r >= 8 of the second)
+  const int half = r / COLS, col = COLS * ct + r % COLS, qj = col / a.G, h = kh * a.G + col % a.G;
   const int vis = col < cols ? max(0, s.len - s.nq + qj + 1) : 0;
-  const int jmin = 16 * ct / a.G, jmax = min(s.rows - 1, (16 * ct + 15) / a.G);
+  const int jmin = COLS * ct / a.G, jmax = min(s.rows - 1, (COLS * ct + COLS - 1) / a.G);
   const int all = max(0, s.len - s.nq + jmin + 1);      // visible to every column
   const int end = max(0, s.len - s.nq + jmax + 1);      // to any
   const int p0 = sp * a.chunk_few, p1 = min(end, p0 + a.chunk_few);
@@ -263,34 +304,34 @@ attn_pages_few_k(AttnPages a) {
   for (int n = 0; n < NG; ++n) psum[n] = f4{0.f, 0.f, 0.f, 0.f};
   const h8 ones = h8(1);
 
-  // the wave's blocks are p0 + 32 (wave + W i); lane 2 i + j holds the page of
-  // tile j of block i, 32 blocks at a time
+  // the wave's blocks are p0 + KEYS (wave + W i); lane T i + j holds the page of
+  // tile j of block i, 64 / T blocks at a time
   const int32_t* row = a.c.table + si * a.c.stride;
-  const int step = W * kBlockKeys;
-  int pages = -1, block = 32;
-  uint32_t valid = 0;  // bit 2 s + j: tile j in slot s is a page's
+  const int step = W * KEYS;
+  int pages = -1, block = 64 / T;
+  uint32_t valid = 0;  // bit T s + j: tile j in slot s is a page's
   const auto issue = [&](int p, int slot) {
-    if (block == 32) {
+    if (block == 64 / T) {
       block = 0;
-      const int64_t pos = (int64_t)p + (lane >> 1) * step + 16 * (lane & 1);
+      const int64_t pos = (int64_t)p + lane / T * step + 16 * (lane % T);
       pages = pos < p1 ? row[pos >> a.c.ps_log2] : -1;
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int page = __builtin_amdgcn_readlane(pages, 2 * block + j);
+    for (int j = 0; j < T; ++j) {
+      const int page = __builtin_amdgcn_readlane(pages, T * block + j);
       const bool ok = page >= 0 && page < a.c.n_pages;
-      valid = (valid & ~(1u << (2 * slot + j))) | ((uint32_t)ok << (2 * slot + j));
+      valid = (valid & ~(1u << (T * slot + j))) | ((uint32_t)ok << (T * slot + j));
       issue_tile<D>(tile_at<D>(a.c, ok ? page : 0, kh, p + 16 * j),
                     ring + slot * BLK + j * kTileBytes<D>, lane);
     }
     ++block;
   };
 
-  int p = p0 + wave * kBlockKeys, slot = 0;
+  int p = p0 + wave * KEYS, slot = 0;
   if (p < p1) issue(p, 0);
   if (p + step < p1) issue(p + step, 1);
 
-  h8 qf[KK];
+  h8 qf[PACK][KK];  // of the column in its own half, 0 in the other
   float qsum[NG];  // of the column's q
   f4 init[NG];     // less q times the codes' bias
 #pragma unroll
@@ -298,12 +339,14 @@ attn_pages_few_k(AttnPages a) {
     float bias = 0.f, sum = 0.f;
 #pragma unroll
     for (int kk = 2 * n; kk < 2 * n + 2; ++kk) {
-      qf[kk] = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
+      const h8 q = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        sum += (float)qf[kk][j];
-        bias += kKBias(j) * (float)qf[kk][j];
+        sum += (float)q[j];
+        bias += kKBias(j) * (float)q[j];
       }
+#pragma unroll
+      for (int u = 0; u < PACK; ++u) qf[u][kk] = half == u ? q : zero_h8();
     }
     qsum[n] = cols_sum(sum);
     bias = cols_sum(bias);
@@ -312,20 +355,29 @@ attn_pages_few_k(AttnPages a) {
 
   const auto compute = [&](int p, int slot, auto edge_c) {
     constexpr bool EDGE = decltype(edge_c)::value;
-    const uint32_t codes = ring_at + slot * BLK + lane * (D / 8), scales = ring_at + slot * BLK + g * (D / 4);
-    // keys of the tiles that exist
-    const int l0 = valid >> (2 * slot) & 1 ? p1 - p : 0;
-    const int l1 = valid >> (2 * slot + 1) & 1 ? p1 - p - 16 : 0;
+    const uint32_t codes = ring_at + slot * BLK + lane * (D / 8);
+    const uint32_t scales = ring_at + slot * BLK + half * (2 * kTileBytes<D>) + g * (D / 4);
+    const int pos = p + 32 * half;  // of this lane's scores
+    int lim[2];                     // keys of its tiles that exist
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      lim[j] = EDGE && !(valid >> (T * slot + 2 * half + j) & 1) ? 0 : p1 - pos - 16 * j;
     float x[2][4], bm = -INFINITY;
     Part<D> t;
+    uint32_t c2[2][KK];  // the second half's codes
     read_part<D, 0, 16 * D>(t, codes, scales);
+    if constexpr (PACK == 2) read_codes<D, 2 * kTileBytes<D>>(c2, codes);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       f4 sc[NG];
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        sc[n] = mfma16(k_codes(t.c[j][2 * n], mg), qf[2 * n], init[n]);
-        sc[n] = mfma16(k_codes(t.c[j][2 * n + 1], mg), qf[2 * n + 1], sc[n]);
+        sc[n] = init[n];
+#pragma unroll
+        for (int kk = 2 * n; kk < 2 * n + 2; ++kk) {
+          sc[n] = mfma16(k_codes(t.c[j][kk], mg), qf[0][kk], sc[n]);
+          if constexpr (PACK == 2) sc[n] = mfma16(k_codes(c2[j][kk], mg), qf[1][kk], sc[n]);
+        }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -338,7 +390,7 @@ attn_pages_few_k(AttnPages a) {
         }
         if constexpr (EDGE) {
           const int key = 4 * g + e;
-          v = key < (j ? l1 : l0) && p + 16 * j + key < vis ? v : -INFINITY;
+          v = key < lim[j] && pos + 16 * j + key < vis ? v : -INFINITY;
         }
         x[j][e] = v;
         bm = fmaxf(bm, v);
@@ -346,6 +398,7 @@ attn_pages_few_k(AttnPages a) {
     }
     uint32_t top = 0;
     read_part<D, 8 * D, 17 * D>(t, codes, scales);
+    if constexpr (PACK == 2) read_codes<D, 2 * kTileBytes<D> + 8 * D>(c2, codes);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -353,7 +406,7 @@ attn_pages_few_k(AttnPages a) {
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
           uint32_t& w = t.pair[j][e * NG + n];
-          if constexpr (EDGE) w = 4 * g + e < (j ? l1 : l0) ? w : 0u;  // past the end: anything
+          if constexpr (EDGE) w = 4 * g + e < lim[j] ? w : 0u;  // past the end: anything
           top = max(top, w);
         }
     bm = cols_max(bm);
@@ -399,14 +452,23 @@ attn_pages_few_k(AttnPages a) {
       psum[n] = mfma16(ones, lo[n], psum[n]);
     }
 #pragma unroll
-    for (int w = 0; w < KK; ++w) {
-      const int n = w / 2;
-      const h8 v0 = v_codes<0>(t.c[0][w], t.c[1][w], mg),
-               v1 = v_codes<1>(t.c[0][w], t.c[1][w], mg);
-      acc[2 * w] = mfma16(v0, hi[n], acc[2 * w]);
-      acc[2 * w] = mfma16(v0, lo[n], acc[2 * w]);
-      acc[2 * w + 1] = mfma16(v1, hi[n], acc[2 * w + 1]);
-      acc[2 * w + 1] = mfma16(v1, lo[n], acc[2 * w + 1]);
+    for (int u = 0; u < PACK; ++u) {
+      h8 phi[NG], plo[NG];  // the half block's weights in its own columns
+#pragma unroll
+      for (int n = 0; n < NG; ++n) {
+        phi[n] = PACK == 1 || half == u ? hi[n] : zero_h8();
+        plo[n] = PACK == 1 || half == u ? lo[n] : zero_h8();
+      }
+#pragma unroll
+      for (int w = 0; w < KK; ++w) {
+        const int n = w / 2;
+        const uint32_t w0 = u ? c2[0][w] : t.c[0][w], w1 = u ? c2[1][w] : t.c[1][w];
+        const h8 v0 = v_codes<0>(w0, w1, mg), v1 = v_codes<1>(w0, w1, mg);
+        acc[2 * w] = mfma16(v0, phi[n], acc[2 * w]);
+        acc[2 * w] = mfma16(v0, plo[n], acc[2 * w]);
+        acc[2 * w + 1] = mfma16(v1, phi[n], acc[2 * w + 1]);
+        acc[2 * w + 1] = mfma16(v1, plo[n], acc[2 * w + 1]);
+      }
     }
   };
 
@@ -414,9 +476,9 @@ attn_pages_few_k(AttnPages a) {
   const auto run = [&](auto edge_c) {
     constexpr bool EDGE = decltype(edge_c)::value;
     for (; p < p1; p += step, slot ^= 1) {
-      if (!EDGE && (p + kBlockKeys > all || (valid >> (2 * slot) & 3) != 3)) return;
+      if (!EDGE && (p + KEYS > all || (valid >> (T * slot) & ((1 << T) - 1)) != (1 << T) - 1)) return;
       if (p + step < p1)  // this block has landed, the next may still travel
-        __builtin_amdgcn_s_waitcnt(waitcnt_imm(2 * kTileLoads<D>, false));
+        __builtin_amdgcn_s_waitcnt(waitcnt_imm(T * kTileLoads<D>, false));
       else
         __builtin_amdgcn_s_waitcnt(waitcnt_imm(0, false));
       __builtin_amdgcn_sched_barrier(0);
@@ -428,7 +490,8 @@ attn_pages_few_k(AttnPages a) {
   run(std::false_type{});
   run(std::true_type{});
 
-  // merge the waves: element e of acc[n] is dimension 16 n + 4 g + e of column r
+  // merge the waves (and halves): element e of acc[n] is dimension 16 n + 4 g + e of
+  // column r
   l = cols_sum(l);
 #pragma unroll
   for (int n = 0; n < NG; ++n) msum[n] = cols_sum(msum[n]);
@@ -444,19 +507,21 @@ attn_pages_few_k(AttnPages a) {
     ll[wave][r] = l;
   }
   __syncthreads();
-  for (int c = tid; c < 16 * D; c += W * 64) {
-    const int cr = c / D, dim = c % D, cc = 16 * ct + cr;
+  for (int c = tid; c < COLS * D; c += W * 64) {
+    const int cr = c / D, dim = c % D, cc = COLS * ct + cr;
     if (cc >= cols) break;
-    float Rm = lR[0][cr];
+    float Rm = -INFINITY;
 #pragma unroll
-    for (int w = 1; w < W; ++w) Rm = fmaxf(Rm, lR[w][cr]);
+    for (int w = 0; w < W * PACK; ++w) Rm = fmaxf(Rm, lR[w / PACK][w % PACK * COLS + cr]);
     const float Rs = Rm == -INFINITY ? 0.f : Rm;
     float A = 0.f, L = 0.f;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const float f = __builtin_amdgcn_exp2f(lR[w][cr] - Rs);
-      A = __builtin_fmaf(reinterpret_cast<const float*>(lds + w * (2 * BLK))[cr * ROW + dim], f, A);
-      L = __builtin_fmaf(ll[w][cr], f, L);
+    for (int w = 0; w < W * PACK; ++w) {
+      const int i = w % PACK * COLS + cr;
+      const float f = __builtin_amdgcn_exp2f(lR[w / PACK][i] - Rs);
+      const float* acc_w = reinterpret_cast<const float*>(lds + w / PACK * (2 * BLK));
+      A = __builtin_fmaf(acc_w[i * ROW + dim], f, A);
+      L = __builtin_fmaf(ll[w / PACK][i], f, L);
     }
     put<D>(a, s, kh * a.G + cc % a.G, s.row0 + cc / a.G, sp, ns, dim, A, Rm, L);
   }
@@ -983,22 +1048,24 @@ static int chunk_of(int64_t max_len, int64_t S, int round) {
   return (int)std::max<int64_t>(round, ((max_len + S - 1) / S + round - 1) / round * round);
 }
 
-// Workgroups.  Few columns: four waves where that gives two workgroups a CU,
-// else eight, whose sums meet in LDS, and below one a CU the keys are split as
-// well, 256 at least each and from 768 on (a second kernel costs what 500 keys of
-// a workgroup do).  us, 32/8 heads, four waves against eight: 64 sequences of
-// 544 keys 16.1 against 20.4, 28 of 2100 26.6 against 22.5; 16 of 500 unsplit
-// 9.4, in two 11.0; 4 of 2000 20.1 and in eight 10.7; 1 of 8000 61.7 and in 32
-// 11.0.  Many columns: two teams, one workgroup a CU, up to three workgroups for
-// each, so that all SIMDs have two waves until the CU's last key; one team, two
-// workgroups a CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135
-// us against 155, eight 504 against 466; four over 509 to 4099 keys 150 against
-// 184).  Parts of 512 keys at least where there is not a workgroup for each CU.
-constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
+// Workgroups.  Few columns: eight waves, whose sums meet in LDS, up to a workgroup
+// for each CU, four up to four, then two; below one a CU the keys are split as well,
+// 256 at least each and from 768 on (a second kernel costs what 500 keys of a
+// workgroup do).  us, 32/8 heads: 28 sequences of 2100 keys with eight waves 22,
+// four 27; 64 of 544 20 and 16; 128 of 2048 with four 65, two 60; 16 of 500 unsplit
+// 9.4, in two 11.0; 4 of 2000 20.1 and in eight 10.7; 1 of 8000 61.7 and in 32 11.0.
+// 64 keys at a time from 1024 on (128 of 2048 67 -> 60, 64 of 2048 37.5 -> 33.8),
+// below they leave waves without a block (64 of 544 15.9 -> 17.1).
+// Many columns: two teams, one workgroup a CU, up to three workgroups for each, so
+// that all SIMDs have two waves until the CU's last key; one team, two workgroups a
+// CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135 us against
+// 155, eight 504 against 466; four over 509 to 4099 keys 150 against 184).  Parts of 512 keys at least where there is not a workgroup for each CU.
+constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kPackKeys = 1024, kMinMany = 512;
 
 struct Plan {
   bool few, many;  // sequences that may be of either kind
-  bool wide;       // eight waves for those of few columns
+  int waves;       // of a workgroup for those of few columns
+  bool pack;       // 64 keys at a time for them
   int teams;       // of a workgroup for the others
   int64_t tiles;   // of 128 columns they have at most
   int chunk_few, chunk_many, splits;
@@ -1011,11 +1078,11 @@ static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t ma
   p.few = !p.many || (G <= kFewCols && M < c->n_seq * max_q);
   const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, kFewCols / G));
   // (with many columns about, most of the others have one row)
-  const int64_t wgs =
-      (int64_t)c->n_seq * c->n_kv_heads * (p.many ? col_tiles(1, G, 16) : col_tiles(few_q, G, 16));
-  p.wide = wgs < 2 * kCUs;
+  const int64_t q = p.many ? 1 : few_q, wgs = (int64_t)c->n_seq * c->n_kv_heads * col_tiles(q, G, 16);
+  p.waves = wgs <= kCUs ? 8 : wgs < 4 * kCUs ? 4 : 2;
   p.chunk_few = chunk_of(max_len, max_len < kSplitFew ? 1 : std::min(kCUs / wgs, max_len / kMinFew),
-                         kBlockKeys);
+                         32);
+  p.pack = q * G <= kPackCols && p.chunk_few > kPackKeys;
   p.tiles = std::min(c->n_seq * col_tiles(max_q, G, kManyCols), M * G / kManyCols + c->n_seq);
   // (of n columns above 64, at most n / 64.5)
   static_assert(kManyCols == 2 * kFewCols, "the bound of a sequence's tiles");
@@ -1067,11 +1134,16 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
     // with work all went to one engine in four (28 sequences of 2100 keys among
     // up to 16 rows: 63.8 us, 23 without)
     const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, kFewCols);
-    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), splits(a.chunk_few), (unsigned)((cols + 15) / 16));
-    if (p.wide)
-      launch(attn_pages_few_k<D, 8>, g, dim3(512), 0, st, a);
+    const int64_t tile = p.pack ? kPackCols : 16;
+    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), splits(a.chunk_few),
+                 (unsigned)((cols + tile - 1) / tile));
+    const auto go = [&](auto kernel) { launch(kernel, g, dim3(64 * p.waves), 0, st, a); };
+    if (p.waves == 8)
+      p.pack ? go(attn_pages_few_k<D, 8, 2>) : go(attn_pages_few_k<D, 8, 1>);
+    else if (p.waves == 4)
+      p.pack ? go(attn_pages_few_k<D, 4, 2>) : go(attn_pages_few_k<D, 4, 1>);
     else
-      launch(attn_pages_few_k<D, 4>, g, dim3(256), 0, st, a);
+      p.pack ? go(attn_pages_few_k<D, 2, 2>) : go(attn_pages_few_k<D, 2, 1>);
   }
   if (p.many && p.tiles > 0) {
     const dim3 g((unsigned)(a.c.Hkv * p.tiles), splits(a.chunk_many));

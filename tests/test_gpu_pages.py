@@ -340,6 +340,9 @@ def test_attention_of_many_column_tiles():
 @pytest.mark.parametrize("lens,rows,H,Hkv,split", [
     ([9000], [1], 2, 1, False),              # eight waves
     ([4500] + [1] * 511, [1] * 512, 2, 1, True),    # four waves
+    ([1500] + [1] * 1100, [1] * 1101, 2, 1, True),  # two
+    ([300] + [2] * 1100, [1] * 1101, 2, 1, True),
+    ([1500, 1100, 1061, 1089], [2, 4, 1, 3], 2, 1, False), ([2200, 1], [1, 1], 8, 1, False),
     ([9000], [40], 4, 1, False), ([40000], [17], 8, 1, False), ([40000], [1], 2, 1, True)])
 def test_attention_past_a_waves_page_indices(lens, rows, H, Hkv, split):
     """Waves hold the pages of 32 (64) of their blocks at a time."""
@@ -354,6 +357,27 @@ def test_attention_past_a_waves_page_indices(lens, rows, H, Hkv, split):
     check(got[:len(q)], want, tol, "long")
     err = np.linalg.norm(got[:len(q)].astype(np.float64) - want) / np.linalg.norm(want)
     assert err <= np.sqrt(2 / 3) * HALF * 1.1, err
+
+
+@pytest.mark.parametrize("rows", [1, 4, 60])
+def test_attention_with_holes_in_a_long_row(rows):
+    """Table entries that are no pages here and there in 1500 keys."""
+    rng = np.random.default_rng(15)
+    lens, H, Hkv, D, ps = [1500], 2, 1, 128, 16
+    c = Cache(lens, Hkv, D, ps, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((rows, H * D)) * 0.1).astype(np.float16)
+    holes = [0, 7, 8, 33, 34, 35, 36, 61, 92]
+    t = c.table.copy()
+    t[0, holes] = [-1, c.n_pages, 1 << 30, -5, -1, -1, c.n_pages + 7, -(1 << 31), -1]
+    c.set_table(t)
+    seen = np.arange(1500)[None] <= (1500 - rows + np.arange(rows))[:, None]
+    for i in holes:
+        seen[:, i * ps:(i + 1) * ps] = False
+    o = O.page_attention(q.reshape(rows, H, D), k[0], v[0], seen).reshape(rows, -1)
+    for split in (False, True):
+        got = attend(c, q, [rows], H, split=split)[:rows]
+        check(got, o, HALF * np.abs(o) + 2 * HALF * np.abs(v[0]).max(), "holes")
 
 
 def test_attention_of_equal_shares_that_are_not():

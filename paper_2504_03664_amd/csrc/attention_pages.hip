@@ -264,11 +264,17 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
 // reverse, so the products of both meet in one register, and everything per score
 // is done once for 64 keys.
 template <int D, int W, int PACK>
-__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(PACK == 2 ? 2 : 3))) void
-attn_pages_few_k(AttnPages a) {
+struct FewLds {  // two blocks a wave; the waves' sums at the end
+  __attribute__((aligned(1024))) uint8_t ring[W][2 * 2 * PACK * kTileBytes<D>];
+  float R[W][16], l[W][16];
+};
+
+template <int D, int W, int PACK>
+__device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp, int ct,
+                                            FewLds<D, W, PACK>& lds) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16;
   constexpr int T = 2 * PACK, KEYS = 16 * T, COLS = 16 / PACK;  // tiles and keys of a block, columns
-  const int kh = blockIdx.x % a.c.Hkv, si = blockIdx.x / a.c.Hkv, sp = blockIdx.y, ct = blockIdx.z;
+  const int kh = pair % a.c.Hkv, si = pair / a.c.Hkv;
   const Seq s = sequence(a, si);
   const int cols = s.rows * a.G;
   if (COLS * ct >= cols || cols > a.few_cols) return;
@@ -278,12 +284,9 @@ attn_pages_few_k(AttnPages a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
-  // two blocks a wave; the waves' sums at the end
   constexpr int BLK = T * kTileBytes<D>, ROW = D + 4;
   static_assert(16 * ROW * 4 <= 2 * BLK, "a wave's sums fit its blocks");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[W * 2 * BLK];
-  __shared__ float lR[W][16], ll[W][16];
-  uint8_t* const ring = lds + wave * (2 * BLK);
+  uint8_t* const ring = lds.ring[wave];
   const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)ring;
 
   // this lane's column: keys [0, vis) are visible
@@ -503,8 +506,8 @@ attn_pages_few_k(AttnPages a) {
     *reinterpret_cast<f4*>(reinterpret_cast<float*>(ring) + r * ROW + 16 * n + 4 * g) = v;
   }
   if (g == 0) {
-    lR[wave][r] = R;
-    ll[wave][r] = l;
+    lds.R[wave][r] = R;
+    lds.l[wave][r] = l;
   }
   __syncthreads();
   for (int c = tid; c < COLS * D; c += W * 64) {
@@ -512,16 +515,16 @@ attn_pages_few_k(AttnPages a) {
     if (cc >= cols) break;
     float Rm = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W * PACK; ++w) Rm = fmaxf(Rm, lR[w / PACK][w % PACK * COLS + cr]);
+    for (int w = 0; w < W * PACK; ++w) Rm = fmaxf(Rm, lds.R[w / PACK][w % PACK * COLS + cr]);
     const float Rs = Rm == -INFINITY ? 0.f : Rm;
     float A = 0.f, L = 0.f;
 #pragma unroll
     for (int w = 0; w < W * PACK; ++w) {
       const int i = w % PACK * COLS + cr;
-      const float f = __builtin_amdgcn_exp2f(lR[w / PACK][i] - Rs);
-      const float* acc_w = reinterpret_cast<const float*>(lds + w / PACK * (2 * BLK));
+      const float f = __builtin_amdgcn_exp2f(lds.R[w / PACK][i] - Rs);
+      const float* acc_w = reinterpret_cast<const float*>(lds.ring[w / PACK]);
       A = __builtin_fmaf(acc_w[i * ROW + dim], f, A);
-      L = __builtin_fmaf(ll[w / PACK][i], f, L);
+      L = __builtin_fmaf(lds.l[w / PACK][i], f, L);
     }
     put<D>(a, s, kh * a.G + cc % a.G, s.row0 + cc / a.G, sp, ns, dim, A, Rm, L);
   }
@@ -616,12 +619,32 @@ __device__ __forceinline__ void as_halves(uint32_t (&w)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i]));
 }
 
+// K operands [tile][kk][lane], V operands [pair of tiles][fragment][lane], the
+// (min, scale) words [K, V][tile][key][group] (0 past the end), the largest of
+// each tile's V and which tiles are pages'
+template <int D>
+struct ManyStage {
+  h8 k[kManyKeys / 16][D / 32][64];
+  h8 v[kManyKeys / 32][D / 16][64];
+  uint32_t pair[2][kManyKeys / 16][16 * (D / 64)];
+  uint32_t top[kManyKeys / 16], valid[kManyKeys / 16];
+};
 template <int D, int TEAMS>
-__global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void
-attn_pages_many_k(AttnPages a) {
+struct ManyLds {
+  static constexpr int ROW = D + 4;  // floats of a column's sums, where the teams meet
+  union {
+    ManyStage<D> st[TEAMS][2];
+    float sums[TEAMS - 1 ? kManyCols : 1][ROW];
+  };
+  float2 rl[TEAMS - 1 ? kManyCols : 1];
+};
+
+template <int D, int TEAMS>
+__device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int sp, ManyLds<D, TEAMS>& lds) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16, T = kManyKeys / 16, U = 2;
-  const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y;
-  const Place at = place_of(a, blockIdx.x / a.c.Hkv);
+  using Stage = ManyStage<D>;
+  const int kh = pair % a.c.Hkv;
+  const Place at = place_of(a, pair / a.c.Hkv);
   if (at.seq < 0) return;
   const int si = __builtin_amdgcn_readfirstlane(at.seq);
   const int ct = __builtin_amdgcn_readfirstlane(at.tile);
@@ -635,22 +658,6 @@ attn_pages_many_k(AttnPages a) {
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
 
-  // K operands [tile][kk][lane], V operands [pair of tiles][fragment][lane], the
-  // (min, scale) words [K, V][tile][key][group] (0 past the end), the largest of
-  // each tile's V and which tiles are pages'
-  struct Stage {
-    h8 k[T][KK][64];
-    h8 v[T / 2][NF][64];
-    uint32_t pair[2][T][16 * NG];
-    uint32_t top[T], valid[T];
-  };
-  constexpr int ROW = D + 4;  // floats of a column's sums, where the teams meet
-  union Lds {
-    Stage st[TEAMS][2];
-    float sums[TEAMS - 1 ? kManyCols : 1][ROW];
-  };
-  __shared__ Lds lds;
-  __shared__ float2 lds_rl[TEAMS - 1 ? kManyCols : 1];
   Stage* const st = lds.st[team];
 
   const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
@@ -897,7 +904,7 @@ attn_pages_many_k(AttnPages a) {
 #pragma unroll
       for (int n = 0; n < NF; ++n)
         *reinterpret_cast<f4*>(&lds.sums[c][16 * n + 4 * g]) = acc[u][n];
-      if (g == 0) lds_rl[c] = make_float2(R[u], l[u]);
+      if (g == 0) lds.rl[c] = make_float2(R[u], l[u]);
     }
   }
   if constexpr (TEAMS == 2) {
@@ -906,7 +913,7 @@ attn_pages_many_k(AttnPages a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = 32 * wave + 16 * u + r;
-      const float2 rl = lds_rl[c];
+      const float2 rl = lds.rl[c];
       const float Rn = fmaxf(R[u], rl.x), Rs = Rn == -INFINITY ? 0.f : Rn;
       const float f0 = __builtin_amdgcn_exp2f(R[u] - Rs), f1 = __builtin_amdgcn_exp2f(rl.x - Rs);
       R[u] = Rn;
@@ -949,6 +956,39 @@ attn_pages_many_k(AttnPages a) {
       }
       if (g == 0) a.part_rl[at] = make_float2(R[u], L);
     }
+  }
+}
+
+template <int D, int W, int PACK>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(PACK == 2 ? 2 : 3))) void
+attn_pages_few_k(AttnPages a) {
+  __shared__ FewLds<D, W, PACK> lds;
+  few_columns<D, W, PACK>(a, blockIdx.x, blockIdx.y, blockIdx.z, lds);
+}
+
+template <int D, int TEAMS>
+__global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void
+attn_pages_many_k(AttnPages a) {
+  __shared__ ManyLds<D, TEAMS> lds;
+  many_columns<D, TEAMS>(a, blockIdx.x, blockIdx.y, lds);
+}
+
+// Both, the many columns' workgroups first: these work for longer, and all of them
+// leave half of a CU's LDS and registers to the others.
+template <int D, int PACK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void
+attn_pages_both_k(AttnPages a, int many, int many_splits, int few_splits) {
+  union Lds {
+    ManyLds<D, 1> many;
+    FewLds<D, 4, PACK> few;
+  };
+  __shared__ Lds lds;
+  const int b = blockIdx.x;
+  if (b < many * many_splits) {
+    many_columns<D, 1>(a, b % many, b / many, lds.many);
+  } else {
+    const int i = b - many * many_splits, pairs = a.c.Hkv * a.c.n_seq;
+    few_columns<D, 4, PACK>(a, i % pairs, i / pairs % few_splits, i / pairs / few_splits, lds.few);
   }
 }
 
@@ -1060,10 +1100,18 @@ static int chunk_of(int64_t max_len, int64_t S, int round) {
 // that all SIMDs have two waves until the CU's last key; one team, two workgroups a
 // CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135 us against
 // 155, eight 504 against 466; four over 509 to 4099 keys 150 against 184).  Parts of 512 keys at least where there is not a workgroup for each CU.
+// Both kinds in one launch hide the few columns' loads behind the many columns'
+// matrix products, but leave these one team: worth it where the workgroups for few
+// columns are more than half as many as full tiles of many columns (all sequences but
+// those having one row), or where one team is right anyway.  32/8 heads, one launch
+// against two: 28 sequences of 520 to 2100 keys and two with 509 rows 53 us against
+// 62, 15 and one of up to 4000 39 against 52, 94 and six 141 against 188; 12 and four
+// 175 against 168, three and one of 16000 keys 450 against 273.
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kPackKeys = 1024, kMinMany = 512;
 
 struct Plan {
   bool few, many;  // sequences that may be of either kind
+  bool both;       // in one launch
   int waves;       // of a workgroup for those of few columns
   bool pack;       // 64 keys at a time for them
   int teams;       // of a workgroup for the others
@@ -1092,6 +1140,9 @@ static Plan plan_attn(const pipo_kv_pages* c, int n_heads, int64_t M, int64_t ma
                           kManyKeys);
   if (M >= (1 << 23)) p.chunk_many = chunk_of(max_len, 1, kManyKeys);  // (a grid of M workgroups)
   p.teams = tiles > 3 * kCUs ? 1 : 2;
+  const int64_t full = std::max<int64_t>(0, M - c->n_seq) * n_heads / kManyCols;
+  p.both = p.few && p.tiles > 0 && (p.teams == 1 || 2 * (int64_t)c->n_seq * c->n_kv_heads > full) &&
+           tiles + 8 * wgs < (1 << 23);  // (threads of a grid: 2^31)
   int chunk = p.chunk_few;
   if (p.many) chunk = p.few ? std::min(chunk, p.chunk_many) : p.chunk_many;
   p.splits = (int)std::max<int64_t>(1, (max_len + chunk - 1) / chunk);
@@ -1127,16 +1178,24 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
   const auto splits = [&](int chunk) {
     return (unsigned)std::max(1, (a.max_len + chunk - 1) / chunk);
   };
-  if (p.few) {
-    // Sequences fastest, so that workgroups with nothing to do (columns and
-    // splits that shorter ones lack) come in a row: workgroups go to the shader
-    // engines by turns, and with the column tiles of a sequence side by side those
-    // with work all went to one engine in four (28 sequences of 2100 keys among
-    // up to 16 rows: 63.8 us, 23 without)
-    const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, kFewCols);
-    const int64_t tile = p.pack ? kPackCols : 16;
-    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), splits(a.chunk_few),
-                 (unsigned)((cols + tile - 1) / tile));
+  const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, kFewCols);
+  const int64_t tile = p.pack ? kPackCols : 16, col_tiles_few = (cols + tile - 1) / tile;
+  // Few columns: sequences fastest, so that workgroups with nothing to do (columns and
+  // splits that shorter ones lack) come in a row: workgroups go to the shader engines
+  // by turns, and with the column tiles of a sequence side by side those with work all
+  // went to one engine in four (28 sequences of 2100 keys among up to 16 rows: 63.8
+  // us, 23 without)
+  if (p.both) {
+    const int many = (int)(a.c.Hkv * p.tiles);
+    const dim3 g((unsigned)(many * splits(a.chunk_many) +
+                            a.c.Hkv * a.c.n_seq * splits(a.chunk_few) * col_tiles_few));
+    const auto go = [&](auto kernel) {
+      launch(kernel, g, dim3(256), 0, st, a, many, (int)splits(a.chunk_many),
+             (int)splits(a.chunk_few));
+    };
+    p.pack ? go(attn_pages_both_k<D, 2>) : go(attn_pages_both_k<D, 1>);
+  } else if (p.few) {
+    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), splits(a.chunk_few), (unsigned)col_tiles_few);
     const auto go = [&](auto kernel) { launch(kernel, g, dim3(64 * p.waves), 0, st, a); };
     if (p.waves == 8)
       p.pack ? go(attn_pages_few_k<D, 8, 2>) : go(attn_pages_few_k<D, 8, 1>);
@@ -1145,7 +1204,7 @@ static void launch_attn_pages(const AttnPages& a, const Plan& p, hipStream_t st)
     else
       p.pack ? go(attn_pages_few_k<D, 2, 2>) : go(attn_pages_few_k<D, 2, 1>);
   }
-  if (p.many && p.tiles > 0) {
+  if (p.many && p.tiles > 0 && !p.both) {
     const dim3 g((unsigned)(a.c.Hkv * p.tiles), splits(a.chunk_many));
     if (p.teams == 2)
       launch(attn_pages_many_k<D, 2>, g, dim3(512), 0, st, a);

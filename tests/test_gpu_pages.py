@@ -380,6 +380,27 @@ def test_attention_with_holes_in_a_long_row(rows):
         check(got, o, HALF * np.abs(o) + 2 * HALF * np.abs(v[0]).max(), "holes")
 
 
+@pytest.mark.parametrize("lens,rows,H,Hkv,D,split", [
+    ([400, 30, 1, 90], [150, 1, 1, 3], 8, 2, 128, True),      # both kinds in one launch
+    ([400, 30, 1, 90], [150, 1, 1, 3], 8, 2, 64, False),
+    ([1600, 1300, 2], [80, 1, 2], 8, 2, 128, True),           # both in parts
+    ([900, 30], [300, 1], 8, 1, 128, True),                   # one after the other
+    ([900, 30], [300, 1], 8, 1, 64, False),
+    ([1500] + [3, 1100] * 64, [70] + [1] * 128, 2, 2, 128, True),   # 64 keys at a time
+    ([1500] + [3, 1100] * 64, [70] + [1, 4] * 64, 4, 2, 64, True),
+    ([700] * 25 + [40] * 7, [600] * 25 + [2] * 7, 32, 8, 64, True)])  # tiles for all CUs
+def test_attention_of_many_and_few_rows(lens, rows, H, Hkv, D, split):
+    print(f"attn both lens={lens[:4]} rows={rows[:4]} D={D} split={split}", flush=True)
+    rng = np.random.default_rng(sum(lens) + D)
+    c = Cache(lens, Hkv, D, 16, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 2 * D ** -0.5).astype(np.float16)
+    got = attend(c, q, rows, H, split=split, behind=3)
+    want, tol = want_attention(q, k, v, rows, lens, H, D)
+    check(got[:len(q)], want, tol, "both")
+    assert (got[len(q):] == 9).all()
+
+
 def test_attention_of_equal_shares_that_are_not():
     """As many rows as sequences times max_q, and sequences of fewer rows behind
     which some belong to none."""

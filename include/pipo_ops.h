@@ -296,10 +296,9 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  * the host knows (max_len at most table_stride * page_size).  A length above
  * max_len counts as max_len, a start outside [0, M] as the nearer end, and of a
  * sequence of more than max_q rows those past the max_q-th are left as they were.
- * Keys on
- * an entry of the table that is not a page are not seen, a row that sees no
- * key becomes 0, rows outside q_start[0] .. q_start[n_seq] - 1 are left as
- * they were.
+ * Keys on an entry of the table that is not a page are not seen, a row that
+ * sees no key becomes 0, rows outside q_start[0] .. q_start[n_seq] - 1 are left
+ * as they were.
  *
  * Where there are few sequences their keys are split over workgroups, whose
  * partials go to `workspace` (device, caller-owned, contents arbitrary, 16-byte
@@ -336,7 +335,9 @@ int64_t pipo_op_attn_pages_workspace_bytes(const pipo_kv_pages* cache, int32_t n
  * resize: sequence i gets want[i] tokens (negative: it keeps its length).
  * Pages past ceil(want[i] / page_size) are given up, missing ones are the lowest
  * free pages (those given up in this call included), in order of the
- * sequences.  want[i] = 0 frees a sequence.  If there are too few pages, or a
+ * sequences.  want[i] = 0 frees a sequence.  A sequence cut to end inside a page
+ * that other rows hold too still shares it: what is appended to it there changes
+ * theirs (forks alone never bring this about).  If there are too few pages, or a
  * row is too short, the table and lengths stay what they were and *missing
  * (device) is how many pages were lacking, else 0.
  */

@@ -640,7 +640,8 @@ struct ManyLds {
 };
 
 template <int D, int TEAMS>
-__device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int sp, ManyLds<D, TEAMS>& lds) {
+__device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int sp,
+                                             ManyLds<D, TEAMS>& lds) {
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16, T = kManyKeys / 16, U = 2;
   using Stage = ManyStage<D>;
   const int kh = pair % a.c.Hkv;
@@ -856,6 +857,13 @@ __device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int s
       for (int n = 0; n < NF; ++n) {
 #pragma unroll
         for (int u = 0; u < U; ++u) acc[u][n] = mfma16(vf[n], pf[u][n / 4], acc[u][n]);
+      }
+      // (else these sums sink behind the next block's unpacking, and keep y and vp alive)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        asm volatile("" : "+v"(l[u]));
+#pragma unroll
+        for (int n = 0; n < NG; ++n) asm volatile("" : "+v"(msum[u][n]));
       }
     }
   };
@@ -1099,11 +1107,12 @@ static int chunk_of(int64_t max_len, int64_t S, int round) {
 // Many columns: two teams, one workgroup a CU, up to three workgroups for each, so
 // that all SIMDs have two waves until the CU's last key; one team, two workgroups a
 // CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135 us against
-// 155, eight 504 against 466; four over 509 to 4099 keys 150 against 184).  Parts of 512 keys at least where there is not a workgroup for each CU.
+// 155, eight 504 against 466; four over 509 to 4099 keys 150 against 184).  Parts of
+// 512 keys at least where there is not a workgroup for each CU.
 // Both kinds in one launch hide the few columns' loads behind the many columns'
-// matrix products, but leave these one team: worth it where the workgroups for few
-// columns are more than half as many as full tiles of many columns (all sequences but
-// those having one row), or where one team is right anyway.  32/8 heads, one launch
+// matrix products, but leave these one team: worth it where sequences times key/value
+// heads are more than half of the tiles of many columns (counting one row of each
+// sequence out), or where one team is right anyway.  32/8 heads, one launch
 // against two: 28 sequences of 520 to 2100 keys and two with 509 rows 53 us against
 // 62, 15 and one of up to 4000 39 against 52, 94 and six 141 against 188; 12 and four
 // 175 against 168, three and one of 16000 keys 450 against 273.

@@ -275,13 +275,23 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   constexpr int KK = D / 32, NG = D / 64, NF = D / 16;
   constexpr int T = 2 * PACK, KEYS = 16 * T, COLS = 16 / PACK;  // tiles and keys of a block, columns
   const int kh = pair % a.c.Hkv, si = pair / a.c.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the wave's blocks are p0 + KEYS (wave + W i); lane T i + j holds the page of
+  // tile j of block i, 64 / T blocks at a time, the first of them read beside the
+  // sequence's length
+  const int32_t* row = a.c.table + si * a.c.stride;
+  const int p0 = sp * a.chunk_few, step = W * KEYS;
+  int p = p0 + wave * KEYS;
+  const auto ahead = [&](int p) { return (int64_t)p + lane / T * step + 16 * (lane % T); };
+  const auto entry = [&](int64_t pos, int end) { return pos < end ? row[pos >> a.c.ps_log2] : -1; };
+  int pages = entry(ahead(p), a.max_len), block = 0;
+
   const Seq s = sequence(a, si);
   const int cols = s.rows * a.G;
   if (COLS * ct >= cols || cols > a.few_cols) return;
   const int ns = max(1, (s.len + a.chunk_few - 1) / a.chunk_few);
   if (sp >= ns) return;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
   constexpr int BLK = T * kTileBytes<D>, ROW = D + 4;
@@ -296,7 +306,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   const int jmin = COLS * ct / a.G, jmax = min(s.rows - 1, (COLS * ct + COLS - 1) / a.G);
   const int all = max(0, s.len - s.nq + jmin + 1);      // visible to every column
   const int end = max(0, s.len - s.nq + jmax + 1);      // to any
-  const int p0 = sp * a.chunk_few, p1 = min(end, p0 + a.chunk_few);
+  const int p1 = min(end, p0 + a.chunk_few);
 
   f4 acc[NF];
 #pragma unroll
@@ -307,17 +317,12 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   for (int n = 0; n < NG; ++n) psum[n] = f4{0.f, 0.f, 0.f, 0.f};
   const h8 ones = h8(1);
 
-  // the wave's blocks are p0 + KEYS (wave + W i); lane T i + j holds the page of
-  // tile j of block i, 64 / T blocks at a time
-  const int32_t* row = a.c.table + si * a.c.stride;
-  const int step = W * KEYS;
-  int pages = -1, block = 64 / T;
   uint32_t valid = 0;  // bit T s + j: tile j in slot s is a page's
+  if (ahead(p) >= p1) pages = -1;
   const auto issue = [&](int p, int slot) {
     if (block == 64 / T) {
       block = 0;
-      const int64_t pos = (int64_t)p + lane / T * step + 16 * (lane % T);
-      pages = pos < p1 ? row[pos >> a.c.ps_log2] : -1;
+      pages = entry(ahead(p), p1);
     }
 #pragma unroll
     for (int j = 0; j < T; ++j) {
@@ -330,7 +335,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
     ++block;
   };
 
-  int p = p0 + wave * KEYS, slot = 0;
+  int slot = 0;
   if (p < p1) issue(p, 0);
   if (p + step < p1) issue(p + step, 1);
 

@@ -263,6 +263,9 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
 // the queries in columns 0..7 and zeros in the others, those of its second 32 the
 // reverse, so the products of both meet in one register, and everything per score
 // is done once for 64 keys.
+// With many sequences bound by HBM (64 of 513 to 544 keys of 56 heads of 128: 274 MB
+// in 66 us, 4.15 TB/s, where a large copy moves 4.86), with few by vector arithmetic
+// (550 instructions for 64 keys) and the loads that wait for each other.
 template <int D, int W, int PACK>
 struct FewLds {  // two blocks a wave; the waves' sums at the end
   __attribute__((aligned(1024))) uint8_t ring[W][2 * 2 * PACK * kTileBytes<D>];
@@ -537,13 +540,16 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
 
 // Many columns: a workgroup is one or two teams of four waves of 32 columns each
 // on (sequence, key/value head, 128 columns, split).  Two teams take the split's
-// keys by turns, 64 at a time, and meet in LDS at the end.  In a team
-// each wave unpacks a tile of the next block into LDS, in operand order (keys as c,
-// values as c - 7.5), while all of them work on this one, so a block is unpacked once for 128
+// keys by turns, 64 at a time, and meet in LDS at the end.  In a team each wave
+// unpacks a tile of the next block into LDS, in operand order (keys as c, values as
+// c - 7.5), while all of them work on this one, so a block is unpacked once for 128
 // columns and every LDS access is a wave's contiguous kilobyte.  The weights p s
 // go to the second product rounded to a half: with the codes centred, and the
 // rest of a value, p (m + 7.5 s), summed in fp32, that is one rounding of the
 // size of the output's own.
+// Bound by vector instructions, 590 of a wave beside 64 matrix ones for a block
+// (eight sequences of 509 rows over 4099 keys, 32/8 heads: 452 us, 567 TFLOP/s, the
+// vector pipe issues in 67 % of the cycles, the matrix pipe is busy in 23 %).
 constexpr int kManyCols = 128, kManyKeys = 64;
 
 // a word of K codes -> eight dimensions, c
@@ -1111,16 +1117,16 @@ static int chunk_of(int64_t max_len, int64_t S, int round) {
 // below they leave waves without a block (64 of 544 15.9 -> 17.1).
 // Many columns: two teams, one workgroup a CU, up to three workgroups for each, so
 // that all SIMDs have two waves until the CU's last key; one team, two workgroups a
-// CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 135 us against
-// 155, eight 504 against 466; four over 509 to 4099 keys 150 against 184).  Parts of
-// 512 keys at least where there is not a workgroup for each CU.
+// CU, beyond (32/8 heads, 509 rows over 4099 keys: two sequences 128 us with two
+// teams, 163 with one; eight 495 and 452; four over 509 to 4099 keys 141 and 171).
+// Parts of 512 keys at least where there is not a workgroup for each CU.
 // Both kinds in one launch hide the few columns' loads behind the many columns'
 // matrix products, but leave these one team: worth it where sequences times key/value
 // heads are more than half of the tiles of many columns (counting one row of each
-// sequence out), or where one team is right anyway.  32/8 heads, one launch
-// against two: 28 sequences of 520 to 2100 keys and two with 509 rows 53 us against
-// 62, 15 and one of up to 4000 39 against 52, 94 and six 141 against 188; 12 and four
-// 175 against 168, three and one of 16000 keys 450 against 273.
+// sequence out), or where one team is right anyway.  32/8 heads, one launch against
+// two: 28 sequences of 520 to 2100 keys and two with 509 rows 52 us and 60, 15 and
+// one of up to 4000 38 and 51, 94 and six 140 and 186; 12 and four 172 and 165, three
+// and one of 16000 keys 439 and 268.
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kPackKeys = 1024, kMinMany = 512;
 
 struct Plan {

@@ -5,7 +5,7 @@
 // a head, eight pairs each, so the sum of squares is three (two) DPP moves and
 // the pairs never leave a lane.  Bound by HBM: each element is read and written
 // once, cos and sin come from the caches (8192 rows of 32 + 8 heads of 128: 168 MB
-// in 33.5 us, where a large copy moves 4.86 TB/s), and by the launch for a decode
+// in 37.5 us, 4.5 TB/s, where a large copy moves 4.86), and by the launch for a decode
 // step (16 rows: 3.2 us).
 #include <algorithm>
 

@@ -909,3 +909,41 @@ def test_streams_and_graphs():
         s.attend(o, stream)
         hip("hipStreamSynchronize", stream)
         assert np.array_equal(o.to_array(np.float16, (n, H * D)), got)
+
+
+def test_a_graph_of_prompts_and_single_tokens():
+    """One captured call whose rows are shared out anew before each replay: prompts
+    beside single tokens, single tokens alone, a prompt alone."""
+    hip = Hip()
+    rng = np.random.default_rng(21)
+    lens, H, Hkv, D = [900, 40, 300, 1, 1300], 8, 2, 128
+    n, M, top, max_q = len(lens), 160, 1300, 150
+    c = Cache(lens, Hkv, D, 32, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((M, H * D)) * 0.2).astype(np.float16)
+    nb = B.pipo_op_attn_pages_workspace_bytes(c.c(), H, M, max_q, top)
+    dq, do, ws = dev(q), DB(M * H * D * 2), DB(max(nb, 16))
+    start, length = DB((n + 1) * 4), dev(np.array(lens, np.int32))
+    stream = hip.stream()
+
+    def put(buf, a):
+        B._check(B.lib().pipo_copy_h2d(buf.ptr, a.ctypes.data, a.nbytes), "pipo_copy_h2d")
+
+    def run(s):
+        B.pipo_op_attn_pages(c.c(), 0, dq.ptr, H * D, start.ptr, length.ptr, do.ptr, H * D, H, M, max_q,
+                             top, ws.ptr, nb, s)
+
+    graph = hip.capture(stream, lambda: run(stream))
+    for rows in ([150, 1, 1, 1, 1], [1] * 5, [0, 0, 0, 0, 150], [30, 40, 3, 0, 80], [150, 1, 1, 1, 1]):
+        put(start, np.concatenate([[0], np.cumsum(rows)]).astype(np.int32))
+        put(do, np.full((M, H * D), 9, np.float16))
+        hip("hipGraphLaunch", graph, stream)
+        hip("hipStreamSynchronize", stream)
+        got = do.to_array(np.float16, (M, H * D))
+        want, tol = want_attention(q, k, v, rows, lens, H, D)
+        check(got[:sum(rows)], want, tol, rows)
+        assert (got[sum(rows):] == 9).all()
+        put(do, np.full((M, H * D), 9, np.float16))
+        run(stream)
+        hip("hipStreamSynchronize", stream)
+        assert np.array_equal(do.to_array(np.float16, (M, H * D)), got)

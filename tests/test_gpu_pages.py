@@ -152,7 +152,8 @@ def draw_rows(lens, width, rng, std=1.0):
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("M,H,Hkv,D,shift,pad", [
     (1, 1, 1, 128, 0, 0), (3, 6, 2, 64, 0, 8), (17, 5, 5, 128, 1, 3), (40, 8, 1, 64, 0, 0),
-    (33, 32, 8, 128, 0, 16), (700, 40, 8, 128, 0, 0), (900, 12, 12, 64, 3, 1)])
+    (33, 32, 8, 128, 0, 16), (700, 40, 8, 128, 0, 0), (900, 12, 12, 64, 3, 1),
+    (3700, 28, 8, 128, 0, 8), (7300, 30, 6, 64, 0, 0)])  # past the L2
 @pytest.mark.parametrize("norm", [True, False])
 def test_norm_rope(M, H, Hkv, D, shift, pad, norm):
     print(f"norm_rope M={M} H={H}/{Hkv} D={D} shift={shift} pad={pad} norm={norm}", flush=True)

@@ -697,9 +697,9 @@ __device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int s
       const int64_t at = (int64_t)pos + (int64_t)lane * (TEAMS * kManyKeys);
       pages = at < p1 ? row[at >> a.c.ps_log2] : -1;
     }
-    lim = p1 - pos;
     const int page = __builtin_amdgcn_readlane(pages, blk & 63);
     ok = page >= 0 && page < a.c.n_pages;
+    lim = ok ? p1 - pos : 0;  // keys of the tile that exist
     const uint8_t* tile = tile_at<D>(a.c, ok ? page : 0, kh, pos);
     load_words(kw, tile + lane * (D / 8));
     load_words(vw, tile + 8 * D + lane * (D / 8));
@@ -719,7 +719,7 @@ __device__ __forceinline__ void many_columns(const AttnPages& a, int pair, int s
       const int at = 4 * (lane % (D / 16));
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if ((at + i) / NG >= lim) pw[i] = 0;  // past the end: anything
+        if ((at + i) / NG >= lim) pw[i] = 0;  // past the end, or page 0's: anything
       *reinterpret_cast<u32x4*>(x.pair[lane / (D / 16)][wave] + at) = pw;
       uint32_t top = max(max(pw[0], pw[1]), max(pw[2], pw[3]));
       top = max(top, lane_move_u<0xB1>(top));

@@ -1,0 +1,73 @@
+"""What attention over a paged 4-bit cache must not read, and how far it may be
+off, where the bounds of test_gpu_pages.py have room: there the error of a score
+is that of codes held 256 above their value, and of the largest query and scale
+of a batch."""
+import numpy as np
+import pytest
+
+from oracle import pages as O
+from paper_2504_03664_amd import binding as B
+from test_gpu_pages import HALF, Cache, attend, check, draw_rows
+
+pytestmark = pytest.mark.gpu
+
+
+class CacheWithoutPage0(Cache):
+    """No sequence holds page 0: whatever it contains is no key's or value's."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        spare = min(set(range(1, self.n_pages)) - set(self.table.reshape(-1).tolist()))
+        t = self.table.copy()
+        t[t == 0] = spare
+        self.set_table(t)
+
+    def set_page0(self, byte):
+        x = np.full(self.page, byte, np.uint8)
+        B._check(B.lib().pipo_copy_h2d(self.pool.ptr, x.ctypes.data, x.nbytes), "pipo_copy_h2d")
+
+
+@pytest.mark.parametrize("lens,rows,H,Hkv,D", [
+    ([1500], [1], 2, 1, 128), ([1500], [4], 2, 1, 64), ([300, 700], [1, 3], 40, 2, 64),
+    ([1500], [60], 2, 1, 128), ([1500], [60], 2, 1, 64), ([1500], [300], 4, 2, 128),
+    ([900, 40, 700, 300], [150, 1, 1, 30], 8, 2, 128),        # both kinds in one launch
+    ([900, 40, 700, 300], [150, 1, 1, 30], 8, 2, 64),
+    ([400] * 12, [130] * 12, 64, 8, 64)])                     # one team a workgroup
+@pytest.mark.parametrize("split", [True, False])
+def test_attention_reads_nothing_of_a_page_that_is_none(lens, rows, H, Hkv, D, split):
+    """Entries that are no pages, beside a page 0 of no sequence whose bytes are
+    NaNs (255), finite scales and mins of 61280 (0x7B) or zeros: the same bits each
+    time, and those of the keys that there are."""
+    print(f"attn page 0 lens={lens[:4]} rows={rows[:4]} D={D} split={split}", flush=True)
+    rng = np.random.default_rng(sum(lens) + sum(rows) + D)
+    ps = 16
+    c = CacheWithoutPage0(lens, Hkv, D, ps, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((sum(rows), H * D)) * 0.1).astype(np.float16)
+    t, bad, holes = c.table.copy(), [-1, c.n_pages, 1 << 30, -(1 << 31)], []
+    for i, n in enumerate(lens):
+        pages = -(-n // ps)
+        at = np.nonzero(rng.random(pages) < 0.2)[0]
+        if pages > 4:
+            at = np.union1d(at, [0, pages // 2])
+        t[i, at] = [bad[x % 4] for x in range(len(at))]
+        holes.append(at)
+    c.set_table(t)
+    got = []
+    for byte in (255, 0x7B, 0):
+        c.set_page0(byte)
+        got.append(attend(c, q, rows, H, split=split)[:len(q)])
+    at = 0
+    for i, (r, n) in enumerate(zip(rows, lens)):
+        seen = np.arange(n)[None] <= (n - r + np.arange(r))[:, None]
+        for j in holes[i]:
+            seen[:, j * ps:(j + 1) * ps] = False
+        x = q[at:at + r].reshape(r, H, D)
+        o = O.page_attention(x, k[i], v[i], seen).reshape(r, -1)
+        # the output's rounding and, of many columns, the weights' (2^-11 of values
+        # of at most max|V|); the errors of scores are below 2^-13
+        tol = HALF * np.abs(o) + 1.25 * HALF * np.abs(v[i]).max() + 2.0 ** -25
+        for y in got:
+            check(y[at:at + r], o, tol, (i, "page 0"))
+        at += r
+    assert np.array_equal(got[0], got[2]) and np.array_equal(got[1], got[2])

@@ -39,6 +39,7 @@ struct AttnPages {
 // max_q equal shares, which saves a launch.
 constexpr int kFewCols = 64;
 constexpr int kPackCols = 8;  // columns with which 64 keys at a time can be taken
+constexpr int kCentreBlocks = 32;  // after which attn_pages_few_k centres its sums
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^15 / (a bound of the block's value scales), so that p s fits a
@@ -93,17 +94,18 @@ __device__ __forceinline__ h8 k_codes(uint32_t w, const Magic& g) {
   return __builtin_bit_cast(h8, o);
 }
 constexpr float kKBias(int j) { return (j / 2) % 2 ? 16.f : 256.f; }
-// V words of two tiles -> the eight keys' codes of dimension 32 w + r (half 0:
-// 256 + c) or 32 w + 16 + r (half 1: 16 + c); key order 0, 2, 1, 3 in each tile
-constexpr float kVBias(int half) { return half ? 16.f : 256.f; }
+// codes as subnormal halves: nibble bits 4..7 of a half are c 2^-20, which the
+// matrix instructions take as it is
+constexpr float kCodeUnit = 0x1p-20f;
+// V words of two tiles -> the eight keys' codes of dimension 32 w + r (half 0) or
+// 32 w + 16 + r (half 1); key order 0, 2, 1, 3 in each tile
 template <int HALF>
-__device__ __forceinline__ h8 v_codes(uint32_t w0, uint32_t w1, const Magic& g) {
-  const uint32_t m = HALF ? g.m16 : g.m256, e = HALF ? g.e16 : g.e256;
+__device__ __forceinline__ h8 v_codes(uint32_t w0, uint32_t w1, uint32_t nibble) {
   u32x4 o;
-  o[0] = ((w0 << 2) & m) | e;
-  o[1] = ((w0 >> 6) & m) | e;
-  o[2] = ((w1 << 2) & m) | e;
-  o[3] = ((w1 >> 6) & m) | e;
+  o[0] = (HALF ? w0 : w0 << 4) & nibble;
+  o[1] = (HALF ? w0 >> 8 : w0 >> 4) & nibble;
+  o[2] = (HALF ? w1 : w1 << 4) & nibble;
+  o[3] = (HALF ? w1 >> 8 : w1 >> 4) & nibble;
   return __builtin_bit_cast(h8, o);
 }
 
@@ -263,6 +265,11 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
 // the queries in columns 0..7 and zeros in the others, those of its second 32 the
 // reverse, so the products of both meet in one register, and everything per score
 // is done once for 64 keys.
+// The sums of p s c, c 0 to 15, grow with the keys where the output does not, and so
+// would their rounding: every kCentreBlocks blocks they are centred.  Relative error
+// of the output over 16384, 65536 and 262144 nearly equal weights (its own rounding:
+// 2e-4): 2.1e-4, 2.1e-4 and 1.8e-4; sums of p s (256 + c), corrected at the end, leave 1.4e-3, 3.7e-3 and
+// 9.2e-3.
 // With many sequences bound by HBM (64 of 513 to 544 keys of 56 heads of 128: 274 MB
 // in 66 us, 4.15 TB/s, where a large copy moves 4.86), with few by vector arithmetic
 // (550 instructions for 64 keys) and the loads that wait for each other.
@@ -297,6 +304,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   if (sp >= ns) return;
   const int r = lane & 15, g = lane >> 4;
   const Magic mg = magic();
+  const uint32_t nibble = sgpr_const(0x00F000F0u);
   constexpr int BLK = T * kTileBytes<D>, ROW = D + 4;
   static_assert(16 * ROW * 4 <= 2 * BLK, "a wave's sums fit its blocks");
   uint8_t* const ring = lds.ring[wave];
@@ -315,7 +323,8 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
 #pragma unroll
   for (int n = 0; n < NF; ++n) acc[n] = f4{0.f, 0.f, 0.f, 0.f};
   float R = -INFINITY, l = 0.f, msum[NG] = {};  // sums of p and p m
-  f4 psum[NG];                                  // of p s, in every element
+  f4 psum[NG];                                  // of p s, in every element, since
+  int blocks = 0;                               // so many blocks
 #pragma unroll
   for (int n = 0; n < NG; ++n) psum[n] = f4{0.f, 0.f, 0.f, 0.f};
   const h8 ones = h8(1);
@@ -474,13 +483,29 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
       for (int w = 0; w < KK; ++w) {
         const int n = w / 2;
         const uint32_t w0 = u ? c2[0][w] : t.c[0][w], w1 = u ? c2[1][w] : t.c[1][w];
-        const h8 v0 = v_codes<0>(w0, w1, mg), v1 = v_codes<1>(w0, w1, mg);
+        const h8 v0 = v_codes<0>(w0, w1, nibble), v1 = v_codes<1>(w0, w1, nibble);
         acc[2 * w] = mfma16(v0, phi[n], acc[2 * w]);
         acc[2 * w] = mfma16(v0, plo[n], acc[2 * w]);
         acc[2 * w + 1] = mfma16(v1, phi[n], acc[2 * w + 1]);
         acc[2 * w + 1] = mfma16(v1, plo[n], acc[2 * w + 1]);
       }
     }
+  };
+
+  // 7.5 p s from the sums of p s c to those of p m (a quarter of it in each of a
+  // column's lanes): both then have values' own size, not that of 7.5 scales
+  const auto centre = [&] {
+#pragma unroll
+    for (int n = 0; n < NF; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        acc[n][e] = __builtin_fmaf(-7.5f * kCodeUnit, psum[n / 4][e], acc[n][e]);
+#pragma unroll
+    for (int n = 0; n < NG; ++n) {
+      msum[n] = __builtin_fmaf(1.875f, psum[n][0], msum[n]);
+      psum[n] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    blocks = 0;
   };
 
   // first the blocks that every column sees whole, up to one without a page
@@ -496,6 +521,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
       compute(p, slot, edge_c);
       __builtin_amdgcn_sched_barrier(0);  // (the slot is read)
       if (p + 2 * step < p1) issue(p + 2 * step, slot);
+      if (++blocks == kCentreBlocks) centre();
     }
   };
   run(std::false_type{});
@@ -503,6 +529,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
 
   // merge the waves (and halves): element e of acc[n] is dimension 16 n + 4 g + e of
   // column r
+  centre();
   l = cols_sum(l);
 #pragma unroll
   for (int n = 0; n < NG; ++n) msum[n] = cols_sum(msum[n]);
@@ -510,7 +537,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   for (int n = 0; n < NF; ++n) {
     f4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = acc[n][e] + (msum[n / 4] - kVBias(n % 2) * psum[n / 4][0]);
+    for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf(acc[n][e], 1.f / kCodeUnit, msum[n / 4]);
     *reinterpret_cast<f4*>(reinterpret_cast<float*>(ring) + r * ROW + 16 * n + 4 * g) = v;
   }
   if (g == 0) {

@@ -71,3 +71,31 @@ def test_attention_reads_nothing_of_a_page_that_is_none(lens, rows, H, Hkv, D, s
             check(y[at:at + r], o, tol, (i, "page 0"))
         at += r
     assert np.array_equal(got[0], got[2]) and np.array_equal(got[1], got[2])
+
+
+@pytest.mark.parametrize("lens,H,Hkv,D", [
+    ([16384] + [1] * 1100, 2, 1, 64),      # two waves a workgroup, 64 keys at a time
+    ([16384] + [1] * 1100, 16, 1, 64),     # 32 keys at a time
+    ([16384] + [1] * 1100, 2, 1, 128),
+    ([65536] + [1] * 300, 2, 1, 64),       # four waves
+    ([65536] + [1] * 1100, 4, 1, 64),
+    ([65536], 2, 1, 64), ([65536], 16, 1, 128), ([262144], 2, 1, 64)])
+def test_attention_over_long_contexts_in_one_part(lens, H, Hkv, D):
+    """Weights nearly alike over one part of many keys: the outputs are as small as
+    one over the root of the keys, and sums of magnitudes are hundreds of times
+    larger.  The output's own rounding has an rms of 2^-11 / root 3 of it at most.
+    fp32 sums that stay of its size, of T / 32 terms at most, are off by root(T / 32)
+    roundings of 2^-25, below 2^-18; sums of codes, 7.5 in the mean where a value's
+    deviation is 4.6, over 32 blocks of 32 keys, by 7.5 / 4.6 * 2^-25 * root(1024) *
+    root(32) together, below 2^-16: a tenth of the first, and 2^-13 for any element,
+    leave room for both."""
+    print(f"attn uniform lens={lens[:2]} H={H}/{Hkv} D={D}", flush=True)
+    rng = np.random.default_rng(lens[0] + H + D)
+    c = Cache(lens, Hkv, D, 64, rng)
+    k, v = c.fill(draw_rows(lens, Hkv * D, rng), draw_rows(lens, Hkv * D, rng))
+    q = (rng.standard_normal((len(lens), H * D)) * 0.02).astype(np.float16)
+    got = attend(c, q, [1] * len(lens), H, split=False)[:1].astype(np.float64)
+    o = O.page_attention(q[:1].reshape(1, H, D), k[0], v[0], np.ones((1, lens[0]), bool)).reshape(1, -1)
+    rms = np.sqrt((o * o).mean())
+    assert np.linalg.norm(got - o) <= 1.1 * HALF / np.sqrt(3) * np.linalg.norm(o)
+    check(got, o, HALF * np.abs(o) + 2.0 ** -13 * rms + 2.0 ** -25, "uniform")

@@ -82,21 +82,18 @@ __device__ __forceinline__ Magic magic() {
   return Magic{vgpr_const(0x5C005C00u), vgpr_const(0x4C004C00u), sgpr_const(0x003C003Cu),
                sgpr_const(0x03C003C0u)};
 }
-// a word of K codes -> eight dimensions in order, each 256 + c (dimensions 0,
-// 1, 4, 5) or 16 + c
-__device__ __forceinline__ h8 k_codes(uint32_t w, const Magic& g) {
-  const uint32_t a = w << 2, b = w >> 6;
-  u32x4 o;
-  o[0] = (a & g.m256) | g.e256;
-  o[1] = (a & g.m16) | g.e16;
-  o[2] = (b & g.m256) | g.e256;
-  o[3] = (b & g.m16) | g.e16;
-  return __builtin_bit_cast(h8, o);
-}
-constexpr float kKBias(int j) { return (j / 2) % 2 ? 16.f : 256.f; }
 // codes as subnormal halves: nibble bits 4..7 of a half are c 2^-20, which the
 // matrix instructions take as it is
 constexpr float kCodeUnit = 0x1p-20f;
+// a word of K codes -> eight dimensions in order
+__device__ __forceinline__ h8 k_codes(uint32_t w, uint32_t nibble) {
+  u32x4 o;
+  o[0] = (w << 4) & nibble;
+  o[1] = w & nibble;
+  o[2] = (w >> 4) & nibble;
+  o[3] = (w >> 8) & nibble;
+  return __builtin_bit_cast(h8, o);
+}
 // V words of two tiles -> the eight keys' codes of dimension 32 w + r (half 0) or
 // 32 w + 16 + r (half 1); key order 0, 2, 1, 3 in each tile
 template <int HALF>
@@ -265,14 +262,19 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
 // the queries in columns 0..7 and zeros in the others, those of its second 32 the
 // reverse, so the products of both meet in one register, and everything per score
 // is done once for 64 keys.
+// Codes are operands at their value, as subnormal halves: under an exponent, as 256 + c,
+// the sums would have to be corrected by up to 17 times what is left of them (relative
+// error of the output where scores hardly differ, 4 heads of 128: 2.1e-4 now at
+// scores of 190 and 2.5e-4 at 1800, where those sums left 7.3e-4 and 4.6e-3; for 1 to 2 %
+// of the time, 64 keys' instructions being 32 more).
 // The sums of p s c, c 0 to 15, grow with the keys where the output does not, and so
 // would their rounding: every kCentreBlocks blocks they are centred.  Relative error
 // of the output over 16384, 65536 and 262144 nearly equal weights (its own rounding:
-// 2e-4): 2.1e-4, 2.1e-4 and 1.8e-4; sums of p s (256 + c), corrected at the end, leave 1.4e-3, 3.7e-3 and
-// 9.2e-3.
+// 2e-4): 2.1e-4, 2.1e-4 and 1.8e-4; corrected at the end only, 1.4e-3, 3.7e-3 and 9.2e-3
+// with p s (256 + c).
 // With many sequences bound by HBM (64 of 513 to 544 keys of 56 heads of 128: 274 MB
 // in 66 us, 4.15 TB/s, where a large copy moves 4.86), with few by vector arithmetic
-// (550 instructions for 64 keys) and the loads that wait for each other.
+// (580 instructions for 64 keys) and the loads that wait for each other.
 template <int D, int W, int PACK>
 struct FewLds {  // two blocks a wave; the waves' sums at the end
   __attribute__((aligned(1024))) uint8_t ring[W][2 * 2 * PACK * kTileBytes<D>];
@@ -303,7 +305,6 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   const int ns = max(1, (s.len + a.chunk_few - 1) / a.chunk_few);
   if (sp >= ns) return;
   const int r = lane & 15, g = lane >> 4;
-  const Magic mg = magic();
   const uint32_t nibble = sgpr_const(0x00F000F0u);
   constexpr int BLK = T * kTileBytes<D>, ROW = D + 4;
   static_assert(16 * ROW * 4 <= 2 * BLK, "a wave's sums fit its blocks");
@@ -352,25 +353,19 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
   if (p + step < p1) issue(p + step, 1);
 
   h8 qf[PACK][KK];  // of the column in its own half, 0 in the other
-  float qsum[NG];  // of the column's q
-  f4 init[NG];     // less q times the codes' bias
+  float qsum[NG];  // of the column's q, in units of the codes
 #pragma unroll
   for (int n = 0; n < NG; ++n) {
-    float bias = 0.f, sum = 0.f;
+    float sum = 0.f;
 #pragma unroll
     for (int kk = 2 * n; kk < 2 * n + 2; ++kk) {
       const h8 q = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sum += (float)q[j];
-        bias += kKBias(j) * (float)q[j];
-      }
+      for (int j = 0; j < 8; ++j) sum += (float)q[j];
 #pragma unroll
       for (int u = 0; u < PACK; ++u) qf[u][kk] = half == u ? q : zero_h8();
     }
-    qsum[n] = cols_sum(sum);
-    bias = cols_sum(bias);
-    init[n] = f4{-bias, -bias, -bias, -bias};
+    qsum[n] = cols_sum(sum) * kCodeUnit;
   }
 
   const auto compute = [&](int p, int slot, auto edge_c) {
@@ -382,7 +377,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       lim[j] = EDGE && !(valid >> (T * slot + 2 * half + j) & 1) ? 0 : p1 - pos - 16 * j;
-    float x[2][4], bm = -INFINITY;
+    float x[2][4], bm = -INFINITY;  // scores times kCodeUnit
     Part<D> t;
     uint32_t c2[2][KK];  // the second half's codes
     read_part<D, 0, 16 * D>(t, codes, scales);
@@ -392,11 +387,11 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
       f4 sc[NG];
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
-        sc[n] = init[n];
+        sc[n] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kk = 2 * n; kk < 2 * n + 2; ++kk) {
-          sc[n] = mfma16(k_codes(t.c[j][kk], mg), qf[0][kk], sc[n]);
-          if constexpr (PACK == 2) sc[n] = mfma16(k_codes(c2[j][kk], mg), qf[1][kk], sc[n]);
+          sc[n] = mfma16(k_codes(t.c[j][kk], nibble), qf[0][kk], sc[n]);
+          if constexpr (PACK == 2) sc[n] = mfma16(k_codes(c2[j][kk], nibble), qf[1][kk], sc[n]);
         }
       }
 #pragma unroll
@@ -432,7 +427,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
     bm = cols_max(bm);
     // scales are below 2^(exponent field - 14)
     const float es = cols_max((float)((int)(top >> 26) - 14));
-    const float Rn = fmaxf(R, __builtin_fmaf(bm, kLog2e, es));
+    const float Rn = fmaxf(R, __builtin_fmaf(bm, kLog2e / kCodeUnit, es));
     const float Rs = EDGE && Rn == -INFINITY ? 0.f : Rn;
     const float alpha = __builtin_amdgcn_exp2f(R - Rs);
     R = Rn;
@@ -453,7 +448,7 @@ __device__ __forceinline__ void few_columns(const AttnPages& a, int pair, int sp
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         constexpr int kOrder[4] = {0, 2, 1, 3};  // of v_codes
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], kLog2e, shift));
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j][e], kLog2e / kCodeUnit, shift));
         l += y;
 #pragma unroll
         for (int n = 0; n < NG; ++n) {
@@ -581,8 +576,14 @@ constexpr int kManyCols = 128, kManyKeys = 64;
 
 // a word of K codes -> eight dimensions, c
 __device__ __forceinline__ h8 k_plain(uint32_t w, const Magic& g) {
+  const uint32_t a = w << 2, b = w >> 6;
+  u32x4 o;
+  o[0] = (a & g.m256) | g.e256;
+  o[1] = (a & g.m16) | g.e16;
+  o[2] = (b & g.m256) | g.e256;
+  o[3] = (b & g.m16) | g.e16;
   const h8 bias = {256.f16, 256.f16, 16.f16, 16.f16, 256.f16, 256.f16, 16.f16, 16.f16};
-  return k_codes(w, g) - bias;
+  return __builtin_bit_cast(h8, o) - bias;
 }
 // a V word -> four keys (0, 2, 1, 3) of dimension 32 w + r (half 0) or 32 w + 16
 // + r, c - 7.5

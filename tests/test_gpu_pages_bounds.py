@@ -99,3 +99,48 @@ def test_attention_over_long_contexts_in_one_part(lens, H, Hkv, D):
     rms = np.sqrt((o * o).mean())
     assert np.linalg.norm(got - o) <= 1.1 * HALF / np.sqrt(3) * np.linalg.norm(o)
     check(got, o, HALF * np.abs(o) + 2.0 ** -13 * rms + 2.0 ** -25, "uniform")
+
+
+def alike_keys(n, Hkv, D, rng, size):
+    """Keys of one value each but in sixteen dimensions of a group of 64, where they
+    differ: the same scale and min in each, and 15 steps of it"""
+    base = rng.uniform(-1, 1, (Hkv, D // 64, 64))
+    base[..., 16], base[..., 17] = -1, 1
+    k = np.broadcast_to(base, (n,) + base.shape).copy()
+    k[..., :16] = rng.uniform(-1, 1, k[..., :16].shape)
+    return (k * size).reshape(n, Hkv * D).astype(np.float16)
+
+
+@pytest.mark.parametrize("rows,H,Hkv,D", [(1, 4, 2, 128), (1, 32, 1, 128), (3, 4, 2, 64), (70, 4, 2, 128),
+                                          (70, 4, 2, 64)])
+@pytest.mark.parametrize("size", [8.0, 75.0])
+def test_attention_of_large_scores_that_hardly_differ(rows, H, Hkv, D, size):
+    """Scores of up to thousands whose differences of about one decide.  A score is
+    the sum over groups of s (q . c) + m sum(q) with codes c from 0 to 15: roundings
+    in fp32 of sums up to 15 s sum|q| + |m sum(q)|, by half a step, 2^-24 of that, and
+    2^-24 / root 3 in the rms.  There are four a group (two products of 32 terms, two
+    multiply-adds); an error d of a score changes the output by p d (v - o)."""
+    print(f"attn alike rows={rows} H={H}/{Hkv} D={D} size={size}", flush=True)
+    rng = np.random.default_rng(8)
+    T, G = 200, D // 64
+    c = Cache([T], Hkv, D, 64, rng)
+    k, v = c.fill([alike_keys(T, Hkv, D, rng, size)], draw_rows([T], Hkv * D, rng))
+    q = rng.standard_normal((rows, H, G, 64)) * 4
+    q[..., :16] *= 0.1 / size
+    q = q.reshape(rows, H * D).astype(np.float16)
+    got = attend(c, q, [rows], H)[:rows].astype(np.float64).reshape(rows, H, D)
+    x, kk, vv = q.reshape(rows, H, D).astype(np.float64), *(np.repeat(y[0], H // Hkv, 1) for y in (k, v))
+    s = np.einsum("nhd,thd->nht", x, kk)
+    g, xg = kk.reshape(T, H, G, 64), x.reshape(rows, H, G, 64)
+    mn, sc = g.min(-1), (g.max(-1) - g.min(-1)) / 15
+    top = np.sqrt(np.einsum("nhg,thg->nht", np.abs(xg).sum(-1) ** 2, (15 * sc) ** 2) +
+                  np.einsum("nhg,thg->nht", xg.sum(-1) ** 2, mn ** 2))
+    err = np.sqrt(4 / 3) * 2.0 ** -24 * top
+    p = np.where(np.arange(T)[None] <= (T - rows + np.arange(rows))[:, None], 1.0, 0.0)[:, None] * np.exp(
+        s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    o = np.einsum("nht,thd->nhd", p, vv)
+    off = sum(((p[..., t] * err[..., t])[..., None] * (vv[t] - o)) ** 2 for t in range(T))
+    many = rows * H // Hkv > 64                    # whose weights are rounded as well
+    tol = 1.1 * np.sqrt(2 if many else 1) * HALF / np.sqrt(3) * np.sqrt((o * o).mean()) + np.sqrt(off.mean())
+    assert np.sqrt(((got - o) ** 2).mean()) <= tol

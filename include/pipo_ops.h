@@ -339,7 +339,7 @@ int64_t pipo_op_attn_pages_workspace_bytes(const pipo_kv_pages* cache, int32_t n
  * that other rows hold too still shares it: what is appended to it there changes
  * theirs (forks alone never bring this about).  If there are too few pages, or a
  * row is too short, the table and lengths stay what they were and *missing
- * (device) is how many pages were lacking, else 0.
+ * (device) is how many pages were lacking (2^31 - 1 for more than that), else 0.
  */
 pipo_status pipo_op_kv_pages_resize(const int32_t* table, const int32_t* len, const int32_t* want,
                                     int32_t* table_out, int32_t* len_out, int64_t table_stride,

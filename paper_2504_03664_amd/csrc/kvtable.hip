@@ -145,26 +145,26 @@ __global__ __launch_bounds__(kThreads) void pages_resize_k(TableArgs a, const in
   __shared__ uint32_t bits[kMaxWords];
   __shared__ int before[kThreads], sums[kWaves], grown[kMaxTableSeqs], held[kMaxTableSeqs],
       need[kMaxTableSeqs];
+  __shared__ unsigned long long excess;  // pages wanted past the rows' ends
   const int tid = threadIdx.x, row0 = tid / kRowLanes;
   for (int w = tid; w < (a.n_pages + 31) / 32; w += kThreads) bits[w] = 0;
-  int total = 0, excess = 0;
+  if (tid == 0) excess = 0;
+  int total = 0;
   for (int i0 = 0; i0 < a.n_seq; i0 += kThreads) {
     const int i = i0 + tid;
-    int g = 0, over = 0, n;
+    int g = 0, n;
+    int64_t over = 0;
     if (i < a.n_seq) {
       const int to = want[i], h = pages_of(a, a.len[i]), k = to < 0 ? h : pages_of(a, to);
       held[i] = h;
       need[i] = k;
       g = max(0, k - h);
-      // (at most 2^19 of a sequence: the sum stays below 2^31)
-      if (to > 0)
-        over = (int)min((int64_t)1 << 19, max((int64_t)0, (int64_t)((to - 1) / a.ps + 1) - a.stride));
+      if (to > 0) over = (to - 1) / a.ps + 1 - a.stride;
     }
     const int at = block_scan(g, sums, n);
     if (i < a.n_seq) grown[i] = total + at;
     total += n;
-    block_scan(over, sums, n);
-    excess += n;
+    if (over > 0) atomicAdd(&excess, (unsigned long long)over);
   }
   __syncthreads();
   for (int i = row0; i < a.n_seq; i += kRows)
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void pages_resize_k(TableArgs a, const in
                 [&](int, int page) { mark(bits, page, a.n_pages); });
   Ranks free;
   const int n_free = free_ranks(bits, before, sums, a.n_pages, free);
-  const int short_by = (int)min((int64_t)max(0, total - n_free) + excess, (int64_t)INT32_MAX);
+  const int short_by = (int)min((int64_t)max(0, total - n_free) + (int64_t)excess, (int64_t)INT32_MAX);
   if (tid == 0) *missing = short_by;
   const bool copy = a.table_out != a.table;
   for (int i = row0; i < a.n_seq; i += kRows) {

@@ -1,13 +1,14 @@
-"""What attention over a paged 4-bit cache must not read, and how far it may be
-off, where the bounds of test_gpu_pages.py have room: there the error of a score
-is that of codes held 256 above their value, and of the largest query and scale
-of a batch."""
+"""The paged 4-bit cache where the bounds of test_gpu_pages.py have room: what
+attention must not read and how far it may be off (there the error of a score is
+that of codes held 256 above their value, and of the largest query and scale of a
+batch), and counts of pages that go far past a table."""
 import numpy as np
 import pytest
 
 from oracle import pages as O
 from paper_2504_03664_amd import binding as B
-from test_gpu_pages import HALF, Cache, attend, check, draw_rows
+from paper_2504_03664_amd.binding import DeviceBuffer as DB
+from test_gpu_pages import HALF, Cache, attend, check, dev, draw_rows
 
 pytestmark = pytest.mark.gpu
 
@@ -144,3 +145,30 @@ def test_attention_of_large_scores_that_hardly_differ(rows, H, Hkv, D, size):
     many = rows * H // Hkv > 64                    # whose weights are rounded as well
     tol = 1.1 * np.sqrt(2 if many else 1) * HALF / np.sqrt(3) * np.sqrt((o * o).mean()) + np.sqrt(off.mean())
     assert np.sqrt(((got - o) ** 2).mean()) <= tol
+
+
+@pytest.mark.parametrize("n,width,ps,n_pages", [(1, 1, 16, 1), (3, 4, 16, 9), (15, 7, 16, 100), (17, 3, 16, 50),
+                                                (300, 5, 256, 1500), (1030, 3, 64, 5000),
+                                                (2048, 3, 16, 5000)])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_resize_counts_every_page_that_is_lacking(n, width, ps, n_pages, inplace):
+    """Rows far too short, alone and beside others that grow: up to 2^38 pages."""
+    print(f"resize lacking n={n} width={width} ps={ps}", flush=True)
+    rng = np.random.default_rng(n)
+    t = np.full((n, width), -1, np.int32)
+    t[0, 0] = 0
+    lens = np.zeros(n, np.int32)
+    lens[0] = 5
+    some = np.where(rng.random(n) < 0.5, rng.integers(0, width * ps + 1, n), -1)
+    for want in (np.full(n, 2 ** 31 - 1), np.where(np.arange(n) == n - 1, 2 ** 31 - 1, some),
+                 np.where(np.arange(n) % 7 == 0, width * ps + 1 + ps * 600000, some),
+                 np.full(n, width * ps + 1)):
+        want = want.astype(np.int32)
+        a, b, lack = O.resize(t, lens.tolist(), want.tolist(), n_pages, ps)
+        dt, dl, dw, dm = dev(t), dev(lens), dev(want), dev(np.full(1, 77, np.int32))
+        ot, ol = (dt, dl) if inplace else (DB(t.nbytes), DB(lens.nbytes))
+        B.pipo_op_kv_pages_resize(dt.ptr, dl.ptr, dw.ptr, ot.ptr, ol.ptr, width, n, n_pages, ps, dm.ptr)
+        B.pipo_dev_synchronize()
+        assert lack > 0 and dm.to_array(np.int32, (1,))[0] == min(lack, 2 ** 31 - 1)
+        assert np.array_equal(ol.to_array(np.int32, (n,)), lens)
+        assert np.array_equal(ot.to_array(np.int32, t.shape), t)

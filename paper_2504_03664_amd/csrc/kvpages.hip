@@ -267,7 +267,9 @@ __global__ __launch_bounds__(256) void pages_read_k(PagesView c, const int32_t* 
 
 // page pairs[i][0] onto page pairs[i][1], i < *n_pairs, in every layer; work
 // items of 16 KiB taken in turn by a fixed grid, since the host does not know
-// how many pairs there are; stores past the L2 (45 MB of pages: 23 -> 18.5 us)
+// how many pairs there are.  Stores go past the L2, of a few pages too: 45 MB of pages
+// take 18.5 us, 23 with ordinary stores, and 28 MB 7.4 and 8.5; with the attention that
+// reads the copies next 28 MB take 62.8 and 62.2, 7 MB 19.0 and 19.2.
 constexpr int kCopyBytes = 16384;
 __global__ __launch_bounds__(256) void pages_copy_k(uint8_t* pool, int64_t layer_bytes,
                                                     int64_t page_bytes, int n_layers, int n_pages,

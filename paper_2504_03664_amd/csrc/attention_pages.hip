@@ -43,8 +43,8 @@ constexpr int kCentreBlocks = 32;  // after which attn_pages_few_k centres its s
 constexpr int kMaxSplits = 64;  // a wave's lanes, in attn_pages_merge_k
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^15 / (a bound of the block's value scales), so that p s fits a
-// half with 29 bits of range below the largest (of a head of two groups the smaller
-// scale's have what is left of them: 11 where scales are 2^18 apart)
+// half with 29 bits of range below the largest (where the scales of a block's keys and
+// groups are far apart, the smaller ones' have what is left of them: 11 at 2^18)
 constexpr float kPBits = 15.f;
 
 // a sequence's rows [row0, row0 + nq), how many of them count (up to max_q), and
@@ -273,7 +273,7 @@ __device__ __forceinline__ void put(const AttnPages& a, const Seq& s, int h, int
 // 2e-4): 2.1e-4, 2.1e-4 and 1.8e-4; corrected at the end only, 1.4e-3, 3.7e-3 and 9.2e-3
 // with p s (256 + c).
 // With many sequences bound by HBM (64 of 513 to 544 keys of 56 heads of 128: 274 MB
-// in 66 us, 4.15 TB/s, where a large copy moves 4.86), with few by vector arithmetic
+// in 65 us, 4.2 TB/s, where a large copy moves 4.86), with few by vector arithmetic
 // (580 instructions for 64 keys) and the loads that wait for each other.
 template <int D, int W, int PACK>
 struct FewLds {  // two blocks a wave; the waves' sums at the end

@@ -8,8 +8,10 @@
 // D/8 lanes hold one head's key (or value) of a row, eight elements each; the
 // lanes of one head in sixteen rows follow each other, so that prompts, whose rows
 // are consecutive positions, write whole words of four keys' codes, and a tile's
-// lines from one workgroup.  Bound by the quantizer's arithmetic for prompts, by the
-// launch for a decode step.
+// lines from one workgroup.  For prompts append is bound by the quantizer's arithmetic
+// (4096 rows of 56 heads of 128: vector instructions issue in 76 % of the cycles), read
+// by HBM (150 MB in 28 us, vector instructions in 65 %); for a decode step both by the
+// launch.
 #include "kvpages.h"
 
 #include <algorithm>
@@ -352,7 +354,7 @@ static pipo_status check_rows(const char* what, const pipo_kv_pages* c, const in
 // Sixteen rows at a time, D/8 threads for a head of each, in rows of 2^22 blocks (a
 // launch takes under 2^32 threads in a dimension).  Four heads a thread where that
 // leaves the chip full, eight blocks a CU (4096 rows of 56 heads: append 68 -> 59
-// us, read 43 -> 32, now 47 and 27).
+// us, read 43 -> 32, now 47 and 28).
 constexpr int kRowHeads = 4;
 static bool many_rows(const PagesView& c, int D, int64_t M) {
   return M * 2 * c.Hkv * (D / 8) >= (int64_t)kRowHeads * 256 * 8 * 256;

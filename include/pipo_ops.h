@@ -292,7 +292,7 @@ pipo_status pipo_op_kv_pages_read(const pipo_kv_pages* cache, int32_t layer, con
  * Every key and value is read as code * scale + min; softmax and sums in fp32,
  * the output rounded once to fp16.  Where a sequence may have more than 64 rows
  * times query heads of a key/value head, each weight times a value's scale is
- * rounded to fp16 as well, which adds about as much as half of the output's rounding.
+ * rounded to fp16 as well, which adds up to as much as the output's own rounding.
  *
  * M: rows of q and o; max_q, max_len: bounds of a sequence's rows and keys that
  * the host knows (max_len at most table_stride * page_size).  A length above

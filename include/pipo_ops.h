@@ -377,6 +377,97 @@ pipo_status pipo_op_kv_pages_compact(const int32_t* table, const int32_t* len, i
 pipo_status pipo_op_kv_pages_copy(const pipo_kv_pages* cache, const int32_t* pairs,
                                   const int32_t* n_pairs, int32_t max_pairs, void* stream);
 
+/* --- the same batches over a paged 8-bit KV cache ---
+ *
+ * Pages, tables, lengths and positions are those of pipo_kv_pages above (the calls on
+ * page tables serve both), with 8 bits an element: PIPO_KV8_E4M3, a floating number of
+ * 4 exponent and 3 mantissa bits (largest 448), or PIPO_KV8_INT8, a whole number from
+ * -127 to 127.  Each block of 16 positions of a head has a scale for its keys and one
+ * for its values, a power of two from 2^-15 to 2^7 (E4M3) or from 2^-24 to 2^9 (INT8),
+ * the least with which the block's largest magnitude is in range.  What a code stands for,
+ * code * scale, is then an fp16 number, exactly.  `fmt` is PIPO_KV8_*; layer_bytes at
+ * least n_pages * pipo_kv8_page_bytes; pools on 128 bytes are read fastest.
+ */
+enum { PIPO_KV8_E4M3 = 0, PIPO_KV8_INT8 = 1 };
+typedef struct {
+  void* pool;
+  int64_t layer_bytes;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t n_layers, n_pages, page_size, n_kv_heads, head_dim, n_seq, fmt, reserved0;
+} pipo_kv8_pages;
+
+/* Bytes of a page of one layer: 2 page_size * n_kv_heads * head_dim and, rounded up to
+ * 128, half of page_size * n_kv_heads; 0 for a shape that is not supported. */
+int64_t pipo_kv8_page_bytes(int32_t page_size, int32_t n_kv_heads, int32_t head_dim);
+
+/*
+ * Rows of new keys and values into the pages of `layer`.  Rows q_start[i] ..
+ * q_start[i+1] - 1 of k and v (fp16, n_kv_heads * head_dim elements at k + m * ldk and v + m
+ * * ldv) become the last positions of sequence i, which is then kv_len[i] long, as
+ * pipo_op_attn_pages has it: q_start has n_seq + 1 entries that do not decrease.
+ * Elements are clamped to +-57344 and NaN counts as 0; each becomes the code nearest to
+ * it, half to even.  A block that earlier positions began keeps at least their
+ * scale; where its new rows need a larger one, the codes of the earlier ones are divided
+ * by the ratio and rounded again, half to even (E4M3: exact but for numbers under 2^-6
+ * of the new scale).  Positions of the block past kv_len[i] count as empty.  Rows whose
+ * position is negative or past the table's row, and rows where the table's entry is not a
+ * page, are skipped, as are starts outside [0, M].  Two sequences of a call may not add to
+ * the same page.
+ */
+pipo_status pipo_op_kv8_pages_append(const pipo_kv8_pages* cache, int32_t layer,
+                                     const int32_t* q_start, const int32_t* kv_len,
+                                     const uint16_t* k, int64_t ldk, const uint16_t* v, int64_t ldv,
+                                     int64_t M, void* stream);
+
+/* Position pos[m] of sequence seq[m] to row m of k and v, exactly.  Rows of no
+ * sequence, position or page are left as they were. */
+pipo_status pipo_op_kv8_pages_read(const pipo_kv8_pages* cache, int32_t layer, const int32_t* seq,
+                                   const int32_t* pos, uint16_t* k, int64_t ldk, uint16_t* v,
+                                   int64_t ldv, int64_t M, void* stream);
+
+/* pipo_op_kv_pages_copy for these pages. */
+pipo_status pipo_op_kv8_pages_copy(const pipo_kv8_pages* cache, const int32_t* pairs,
+                                   const int32_t* n_pairs, int32_t max_pairs, void* stream);
+
+/*
+ * What attention makes of a score x = q . k, and which keys a row sees (NULL, or all
+ * zero: x itself, and the keys up to the row's position).  In this order:
+ *   cap > 0:    x becomes cap * tanh(x / cap);
+ *   slopes:     (device fp32 [n_heads], NULL: none) slopes[h] * |row's position - key's| is
+ *               taken from it;
+ *   window > 0: of the keys up to its position a row sees the last `window` alone;
+ *   prefix:     (device int32 [n_seq], NULL: none) every row of sequence i sees keys
+ *               0 .. prefix[i] - 1 as well, whatever its position and window; above
+ *               max_prefix counts as max_prefix, which the host knows.
+ */
+typedef struct {
+  float cap;
+  int32_t window;
+  const float* slopes;
+  const int32_t* prefix;
+  int32_t max_prefix, reserved0;
+} pipo_attn_scores;
+
+/*
+ * pipo_op_attn_pages over these pages, with `scores` (read on the host during the call;
+ * may be NULL).  Everything said there holds: rows and lengths, bounds, what is left as
+ * it was, the workspace (of pipo_op_attn_kv8_pages_workspace_bytes bytes) and the limits.
+ * A row that sees no key becomes 0.  Keys and values are read exactly, softmax and
+ * sums in fp32, the output rounded once to fp16; where a sequence may have more than
+ * 64 rows times query heads of a key/value head, weights are rounded to fp16 as well.
+ */
+pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* cache, int32_t layer,
+                                   const pipo_attn_scores* scores, const uint16_t* q, int64_t ldq,
+                                   const int32_t* q_start, const int32_t* kv_len, uint16_t* o,
+                                   int64_t ldo, int32_t n_heads, int64_t M, int32_t max_q,
+                                   int32_t max_len, void* workspace, int64_t workspace_bytes,
+                                   void* stream);
+/* (pool and table of `cache`, slopes and prefix of `scores` are not read) */
+int64_t pipo_op_attn_kv8_pages_workspace_bytes(const pipo_kv8_pages* cache,
+                                               const pipo_attn_scores* scores, int32_t n_heads,
+                                               int64_t M, int32_t max_q, int32_t max_len);
+
 /* SwiGLU: h[m][i] = silu(gu[m][i]) * gu[m][F + i], silu(g) = g / (1 +
  * exp(-g)), in fp32; gu [M][2F], h [M][F] fp16, F % 8 == 0. */
 pipo_status pipo_op_swiglu(const uint16_t* gu, uint16_t* h, int64_t M, int64_t F, void* stream);
@@ -398,6 +489,34 @@ pipo_status pipo_op_argmax(const float* logits, int32_t* next, int64_t rows, int
 pipo_status pipo_op_argmax_ws(const float* logits, int32_t* next, int64_t rows, int64_t V,
                               void* workspace, int64_t workspace_bytes, void* stream);
 int64_t pipo_op_argmax_workspace_bytes(int64_t rows, int64_t V);
+
+/*
+ * A token for each row of logits (fp32, V of them at logits + r * ld), drawn with a
+ * given random number.  Settings are device arrays [rows], each NULL where no row
+ * has it: temperature T (NULL: 1), top_k, min_p, top_p.  A logit x weighs
+ * exp((x - largest) / T).  Tokens in the order of falling logits, equal ones by index:
+ *   top_k > 0:  the first top_k stay;
+ *   min_p > 0:  of them those that weigh at least min_p (above 1 counts as 1);
+ *   top_p < 1:  of these the first ones until their weights reach top_p of all that
+ *               stayed (one at least);
+ * and next[r] is the first one of the rest with which the weights so far are above
+ * u[r] of the rest's (u in [0, 1); outside, the nearer end).  logprob[r] (NULL: not wanted) is
+ * the logarithm of its share of the rest.
+ * T that is not above 0 (NaN too) takes the largest logit, with logprob 0.  NaN and -infinite
+ * logits are never drawn; of infinite ones alone; a row with nothing else gives 0, and
+ * logprob -infinity.  Weights under e^-31 of the largest count as none.  Weights are
+ * held to 2^-36 of their size and summed as whole numbers, so the result does not depend
+ * on the workspace or on the run.
+ * workspace (device, caller-owned, contents arbitrary, 16-byte aligned) of
+ * pipo_op_sample_workspace_bytes(rows, V) bytes lets several workgroups share a row; with less
+ * (or NULL) one does it all: the same result.  Calls sharing a workspace must not overlap
+ * in time.  V up to 2^23 and rows below 2^22, else PIPO_ERR_UNSUPPORTED.
+ */
+pipo_status pipo_op_sample(const float* logits, int64_t ld, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p,
+                           const float* u, int32_t* next, float* logprob, int64_t rows, int64_t V,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+int64_t pipo_op_sample_workspace_bytes(int64_t rows, int64_t V);
 
 /* Plain device-to-device copy kernel: reads and writes `bytes` once
  * (multiple of 16, 16-byte aligned pointers).  Not part of the decoder: it

@@ -30,6 +30,7 @@ PIPO_W_FP16, PIPO_W_INT4_G64 = 0, 1
 PIPO_FAMILY_OPT, PIPO_FAMILY_LLAMA = 0, 1
 PIPO_LAYOUT_ROW_MAJOR, PIPO_LAYOUT_FRAGMENT = 0, 1
 PIPO_KV_FP16, PIPO_KV_INT4_G64 = 0, 1
+PIPO_KV8_E4M3, PIPO_KV8_INT8 = 0, 1
 PIPO_PIPE_PERFORMANCE, PIPO_PIPE_MEMORY_EFFICIENT = 0, 1
 PIPO_DBG_POISON_SLOTS, PIPO_DBG_COPY_DELAY, PIPO_DBG_TIMESTAMPS = 1, 2, 4
 PIPO_DBG_KV_PAGEABLE, PIPO_DBG_SEGMENT_COPIES, PIPO_DBG_UNFUSED = 8, 16, 32
@@ -102,6 +103,15 @@ class PipoKvPages(ctypes.Structure):
     _fields_ = [("pool", vp), ("layer_bytes", i64), ("table", vp), ("table_stride", i64),
                 ("n_layers", i32), ("n_pages", i32), ("page_size", i32), ("n_kv_heads", i32),
                 ("head_dim", i32), ("n_seq", i32)]
+
+
+class PipoKv8Pages(ctypes.Structure):
+    _fields_ = PipoKvPages._fields_ + [("fmt", i32), ("reserved0", i32)]
+
+
+class PipoAttnScores(ctypes.Structure):
+    _fields_ = [("cap", f32), ("window", i32), ("slopes", vp), ("prefix", vp), ("max_prefix", i32),
+                ("reserved0", i32)]
 
 
 class PipoSchedConfig(ctypes.Structure):
@@ -188,6 +198,19 @@ _SIGNATURES = {
     "pipo_op_kv_pages_fork": ([vp, vp, i32, vp, vp, vp, i32, i64, i32, i32, vp, vp, vp, vp], i32),
     "pipo_op_kv_pages_compact": ([vp, vp, vp, i64, i32, i32, i32, vp, vp, vp], i32),
     "pipo_op_kv_pages_copy": ([ctypes.POINTER(PipoKvPages), vp, vp, i32, vp], i32),
+    "pipo_kv8_page_bytes": ([i32, i32, i32], i64),
+    "pipo_op_kv8_pages_append": ([ctypes.POINTER(PipoKv8Pages), i32, vp, vp, vp, i64, vp, i64, i64,
+                                  vp], i32),
+    "pipo_op_kv8_pages_read": ([ctypes.POINTER(PipoKv8Pages), i32, vp, vp, vp, i64, vp, i64, i64,
+                                vp], i32),
+    "pipo_op_kv8_pages_copy": ([ctypes.POINTER(PipoKv8Pages), vp, vp, i32, vp], i32),
+    "pipo_op_attn_kv8_pages": ([ctypes.POINTER(PipoKv8Pages), i32, ctypes.POINTER(PipoAttnScores), vp,
+                                i64, vp, vp, vp, i64, i32, i64, i32, i32, vp, i64, vp], i32),
+    "pipo_op_attn_kv8_pages_workspace_bytes": ([ctypes.POINTER(PipoKv8Pages),
+                                                ctypes.POINTER(PipoAttnScores), i32, i64, i32, i32],
+                                               i64),
+    "pipo_op_sample": ([vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp], i32),
+    "pipo_op_sample_workspace_bytes": ([i64, i64], i64),
     "pipo_op_swiglu": ([vp, vp, i64, i64, vp], i32),
     "pipo_op_embed": ([vp, vp, vp, vp, i64, i64, i64, i64, i64, vp], i32),
     "pipo_sched_trace": ([ctypes.POINTER(PipoSchedConfig), i32, vp, vp, vp, i64, vp, i64], i64),
@@ -611,6 +634,54 @@ def pipo_op_kv_pages_compact(table, length, table_out, table_stride, n_seq, n_pa
 def pipo_op_kv_pages_copy(cache: PipoKvPages, pairs, n_pairs, max_pairs, stream=None):
     _check(lib().pipo_op_kv_pages_copy(ctypes.byref(cache), pairs, n_pairs, max_pairs, stream),
            "pipo_op_kv_pages_copy")
+
+
+# --- the same over a paged 8-bit KV cache ---
+def pipo_kv8_page_bytes(page_size: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().pipo_kv8_page_bytes(page_size, n_kv_heads, head_dim))
+
+
+def pipo_op_kv8_pages_append(cache: PipoKv8Pages, layer, q_start, kv_len, k, ldk, v, ldv, M,
+                             stream=None):
+    _check(lib().pipo_op_kv8_pages_append(ctypes.byref(cache), layer, q_start, kv_len, k, ldk, v, ldv,
+                                          M, stream), "pipo_op_kv8_pages_append")
+
+
+def pipo_op_kv8_pages_read(cache: PipoKv8Pages, layer, seq, pos, k, ldk, v, ldv, M, stream=None):
+    _check(lib().pipo_op_kv8_pages_read(ctypes.byref(cache), layer, seq, pos, k, ldk, v, ldv, M,
+                                        stream), "pipo_op_kv8_pages_read")
+
+
+def pipo_op_kv8_pages_copy(cache: PipoKv8Pages, pairs, n_pairs, max_pairs, stream=None):
+    _check(lib().pipo_op_kv8_pages_copy(ctypes.byref(cache), pairs, n_pairs, max_pairs, stream),
+           "pipo_op_kv8_pages_copy")
+
+
+def pipo_op_attn_kv8_pages(cache: PipoKv8Pages, layer, scores: Optional[PipoAttnScores], q, ldq,
+                           q_start, kv_len, o, ldo, n_heads, M, max_q, max_len, workspace=None,
+                           workspace_bytes=0, stream=None):
+    _check(lib().pipo_op_attn_kv8_pages(ctypes.byref(cache), layer,
+                                        ctypes.byref(scores) if scores is not None else None, q, ldq,
+                                        q_start, kv_len, o, ldo, n_heads, M, max_q, max_len,
+                                        workspace, workspace_bytes, stream),
+           "pipo_op_attn_kv8_pages")
+
+
+def pipo_op_attn_kv8_pages_workspace_bytes(cache: PipoKv8Pages, scores: Optional[PipoAttnScores],
+                                           n_heads, M, max_q, max_len) -> int:
+    return int(lib().pipo_op_attn_kv8_pages_workspace_bytes(
+        ctypes.byref(cache), ctypes.byref(scores) if scores is not None else None, n_heads, M, max_q,
+        max_len))
+
+
+def pipo_op_sample(logits, ld, temperature, top_k, top_p, min_p, u, nxt, logprob, rows, V,
+                   workspace=None, workspace_bytes=0, stream=None):
+    _check(lib().pipo_op_sample(logits, ld, temperature, top_k, top_p, min_p, u, nxt, logprob, rows, V,
+                                workspace, workspace_bytes, stream), "pipo_op_sample")
+
+
+def pipo_op_sample_workspace_bytes(rows, V) -> int:
+    return int(lib().pipo_op_sample_workspace_bytes(rows, V))
 
 
 def pipo_op_swiglu(gu, h, M, F, stream=None):

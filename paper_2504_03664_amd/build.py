@@ -29,7 +29,8 @@ HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLU
              "-Wno-unused-result"]
 SOURCES = ["gemm.hip", "gemm_slab_f16.hip", "gemm_slab_w4.hip", "attention.hip", "attention_gqa.hip",
            "attention_pages.hip", "kvcache.hip", "kvpages.hip", "kvtable.hip", "norm_rope.hip",
-           "elementwise.hip", "engine.cpp", "config.cpp", "pack.cpp", "ops_api.cpp",
+           "elementwise.hip", "kvpages8.hip",
+           "attention_pages8.hip", "sample.hip", "engine.cpp", "config.cpp", "pack.cpp", "ops_api.cpp",
            "schedule.cpp", "sched_capi.cpp"]
 SCHED_SOURCES = ["schedule.cpp", "sched_capi.cpp"]
 

@@ -45,6 +45,11 @@ __device__ __forceinline__ const uint8_t* tile_at(const PagesView& v, int page, 
          (uint32_t)((head << (v.ps_log2 - 4)) + ((pos >> 4) & (tiles - 1))) * kTileBytes<D>;
 }
 
+// whole pages of every layer, of any format (pages of a multiple of 16 bytes)
+void launch_pages_copy(uint8_t* pool, int64_t layer_bytes, int64_t page_bytes, int n_layers,
+                       int n_pages, const int32_t* pairs, const int32_t* n_pairs, int max_pairs,
+                       hipStream_t st);
+
 pipo_status check_pages(const char* what, const pipo_kv_pages* c, int32_t layer, PagesView* v);
 
 }  // namespace pipo

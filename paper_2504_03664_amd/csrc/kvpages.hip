@@ -303,6 +303,15 @@ __global__ __launch_bounds__(256) void pages_copy_k(uint8_t* pool, int64_t layer
   }
 }
 
+void launch_pages_copy(uint8_t* pool, int64_t layer_bytes, int64_t page_bytes, int n_layers,
+                       int n_pages, const int32_t* pairs, const int32_t* n_pairs, int max_pairs,
+                       hipStream_t st) {
+  const int64_t pieces = (page_bytes + kCopyBytes - 1) / kCopyBytes;
+  const int64_t items = (int64_t)max_pairs * n_layers * pieces;
+  launch(pages_copy_k, dim3((unsigned)std::min<int64_t>(items, 2048)), dim3(256), 0, st, pool,
+         layer_bytes, page_bytes, n_layers, n_pages, pairs, n_pairs, max_pairs);
+}
+
 pipo_status check_pages(const char* what, const pipo_kv_pages* c, int32_t layer, PagesView* v) {
   if (!c || !c->pool || !c->table || reinterpret_cast<uintptr_t>(c->pool) % 16 != 0) {
     set_error("%s: NULL cache, pool or table, or a pool off 16-byte alignment", what);
@@ -452,11 +461,8 @@ pipo_status pipo_op_kv_pages_copy(const pipo_kv_pages* c, const int32_t* pairs,
     return PIPO_ERR_ARG;
   }
   if (max_pairs == 0) return PIPO_OK;
-  const int64_t pieces = (view.page_bytes + kCopyBytes - 1) / kCopyBytes;
-  const int64_t items = (int64_t)max_pairs * c->n_layers * pieces;
-  launch(pages_copy_k, dim3((unsigned)std::min<int64_t>(items, 2048)), dim3(256), 0,
-         static_cast<hipStream_t>(stream), view.pool, c->layer_bytes, view.page_bytes, c->n_layers,
-         c->n_pages, pairs, n_pairs, max_pairs);
+  launch_pages_copy(view.pool, c->layer_bytes, view.page_bytes, c->n_layers, c->n_pages, pairs, n_pairs,
+                    max_pairs, static_cast<hipStream_t>(stream));
   PIPO_HIP_TRY(hipGetLastError());
   return PIPO_OK;
 }

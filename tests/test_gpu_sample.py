@@ -1,0 +1,201 @@
+"""The draw of tokens on the GPU against its definition in 64 bits (oracle/sample.py):
+tokens are equal, and the logarithms are off by the fp32 rounding of the result
+(2^-24 of it) and by what weights held to 2^-36 leave (2^-34)."""
+import numpy as np
+import pytest
+
+from oracle.sample import sample
+from paper_2504_03664_amd import binding as B
+from paper_2504_03664_amd.binding import DeviceBuffer as DB
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a, dtype):
+    return None if a is None else DB.from_array(np.ascontiguousarray(a, dtype))
+
+
+def draw(x, u, T=None, k=None, p=None, m=None, workspace=True, pad=0, shift=0, logprob=True):
+    rows, V = x.shape
+    full = np.full((rows, V + pad), 1e30, np.float32)      # (what is not a row's is never read as one)
+    full[:, :V] = x
+    dx = dev(np.concatenate([np.zeros(shift, np.float32), full.reshape(-1)]), np.float32)
+    args = dev(T, np.float32), dev(k, np.int32), dev(p, np.float32), dev(m, np.float32)
+    du, dn, dl = dev(u, np.float32), dev(np.full(rows + 1, 77), np.int32), dev(np.full(rows + 1, 7.0), np.float32)
+    n = B.pipo_op_sample_workspace_bytes(rows, V) if workspace else 0
+    ws = dev(np.full(max(n // 4, 4), -1), np.int32)
+    B.pipo_op_sample(dx.ptr + 4 * shift, V + pad, *(a.ptr if a else None for a in args), du.ptr, dn.ptr,
+                     dl.ptr if logprob else None, rows, V, ws.ptr if n else None, n)
+    B.pipo_dev_synchronize()
+    nxt, lp = dn.to_array(np.int32, (rows + 1,)), dl.to_array(np.float32, (rows + 1,))
+    assert nxt[-1] == 77 and lp[-1] == 7
+    return nxt[:-1], lp[:-1]
+
+
+def check(x, u, T=None, k=None, p=None, m=None, **kw):
+    got, lp = draw(x, u, T, k, p, m, **kw)
+    one = lambda a, i, other: other if a is None else a[i]  # noqa: E731
+    for i in range(len(x)):
+        f32 = lambda v: float(np.float32(v))  # noqa: E731
+        token, log = sample(x[i], f32(u[i]), f32(one(T, i, 1.0)), int(one(k, i, 0)), f32(one(p, i, 1.0)),
+                            f32(one(m, i, 0.0)))
+        assert got[i] == token, (i, got[i], token, u[i])
+        if kw.get("logprob", True):
+            assert lp[i] == log or abs(float(lp[i]) - log) <= 2.0 ** -24 * abs(log) + 2.0 ** -34, (i, lp[i], log)
+    return got, lp
+
+
+def logits(rng, rows, V, std=2.5):
+    x = (rng.standard_normal((rows, V)) * std).astype(np.float32)
+    if V > 20:
+        x[:, rng.integers(0, V, V // 20)] += 2 * std
+        x[:, rng.integers(1, V, V // 20)] = -np.inf
+    return x
+
+
+WORK = pytest.mark.parametrize("workspace", [True, False])
+
+
+@WORK
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 255, 1000, 8191, 8192, 8193, 50272])
+def test_plain_draw(V, workspace):
+    print(f"sample V={V} workspace={workspace}", flush=True)
+    rng = np.random.default_rng(V)
+    rows = 5
+    check(logits(rng, rows, V), rng.random(rows), workspace=workspace)
+    check(logits(rng, rows, V), rng.random(rows), T=rng.uniform(0.2, 3, rows), workspace=workspace,
+          pad=3, shift=1)
+
+
+@WORK
+@pytest.mark.parametrize("V,std", [(700, 1.0), (9000, 2.5), (30000, 0.3), (20000, 6.0)])
+def test_limits(V, std, workspace):
+    """Each limit alone and all of them, over settings of every row's own."""
+    print(f"sample limits V={V} std={std} workspace={workspace}", flush=True)
+    rng = np.random.default_rng(V)
+    rows = 24
+    x = logits(rng, rows, V, std)
+    u, T = rng.random(rows), rng.uniform(0.3, 2, rows)
+    k = rng.choice([0, 1, 2, 50, 300, 600, V - 1, V, V + 5, -3], rows)
+    p = rng.choice([0.0, 1e-6, 0.1, 0.5, 0.9, 0.99, 0.999999, 1.0, 1.5, -1.0], rows)
+    m = rng.choice([0.0, 1e-9, 1e-4, 0.01, 0.5, 1.0, 2.0, -1.0], rows)
+    check(x, u, T, k=k, workspace=workspace)
+    check(x, u, T, p=p, workspace=workspace)
+    check(x, u, T, m=m, workspace=workspace)
+    check(x, u, T, k, p, m, workspace=workspace)
+    check(x, u, None, k, p, m, workspace=workspace, logprob=False)
+
+
+@WORK
+def test_greedy_and_nothing(workspace):
+    """T of 0, below, NaN; rows of NaN and -infinity; infinite logits; the first of equals."""
+    rng = np.random.default_rng(1)
+    x = logits(rng, 12, 9000)
+    x[0, [5, 8999]] = 40.0
+    x[1] = np.nan
+    x[2] = -np.inf
+    x[3, ::2] = np.nan
+    x[4, [100, 8500]] = np.inf
+    x[5, 3] = np.inf
+    x[6, :] = -np.inf
+    x[6, 8888] = -3e38
+    x[7, :] = 3e38
+    x[8, :] = -1e30
+    x[9, 17] = np.nan
+    u = rng.random(12)
+    for T in (0.0, -1.0, np.nan, -np.inf, 1.0, 0.5, 1e-30, 1e-44, 1e30):
+        check(x, u, T=np.full(12, T), workspace=workspace)
+    T = np.array([0.0, 1, 0.0, 2, 0.7, 0, 1, 1, 0.5, np.nan, 1, -0.0])
+    check(x, u, T=T, k=np.full(12, 3), p=np.full(12, 0.9), m=np.full(12, 0.1), workspace=workspace)
+
+
+@WORK
+def test_infinite_temperature(workspace):
+    """Every finite logit weighs the same."""
+    rng = np.random.default_rng(2)
+    x = logits(rng, 3, 5000)
+    x[:, 7] = -np.inf
+    u = np.array([0.1, 0.55, 0.999])
+    got, lp = draw(x, u, T=np.full(3, np.inf), workspace=workspace)
+    for i in range(3):
+        n = int((x[i] > -np.inf).sum())
+        order = np.lexsort((np.arange(5000), -x[i].astype(np.float64)))
+        assert got[i] == order[int(np.float32(u[i]) * np.float64(n))]
+        assert abs(float(lp[i]) + np.log(n)) <= 2.0 ** -24 * np.log(n) + 2.0 ** -34
+
+
+@WORK
+@pytest.mark.parametrize("V", [4, 513, 8000, 20000])
+def test_equal_logits(V, workspace):
+    """Equal weights go by index, exactly: shares that fall on a border, few and many equals."""
+    rows = 12
+    u = np.array([0, 0.25, 0.5, 0.75, 0.999, 1.0, 0.1, 0.3, 0.6, 0.125, 0.875, 0.5])
+    check(np.full((rows, V), 1.5, np.float32), u, workspace=workspace)
+    x = np.zeros((rows, V), np.float32)
+    x[:, 1::2] = -0.0
+    check(x, u, k=np.full(rows, V // 2), workspace=workspace)
+    check(x, u, p=np.full(rows, 0.5), workspace=workspace)
+    check(x, u, k=np.full(rows, max(V // 2, 2)), p=np.full(rows, 0.25), m=np.ones(rows), workspace=workspace)
+
+
+@WORK
+def test_steps_of_equal_logits(workspace):
+    """Whole-number logits: many equals in a few bins, borders between them."""
+    rng = np.random.default_rng(3)
+    rows, V = 20, 12000
+    x = rng.integers(-8, 9, (rows, V)).astype(np.float32)
+    u = rng.random(rows)
+    check(x, u, workspace=workspace)
+    check(x, u, k=rng.integers(1, V, rows), p=rng.random(rows), workspace=workspace)
+    check(x, u, m=np.exp(-rng.integers(0, 12, rows)) * rng.choice([0.9, 1.1], rows), workspace=workspace)
+
+
+@WORK
+def test_one_bin_of_many_different_logits(workspace):
+    """More tokens within a sixteenth than are put in order at once, all different."""
+    rng = np.random.default_rng(4)
+    rows, V = 10, 20000
+    for base in (0.0, 5.0, -300.0, 1e-3):
+        x = (base + rng.random((rows, V)) * 0.1).astype(np.float32)
+        u = np.concatenate([[0.0, 1.0], rng.random(rows - 2)])
+        check(x, u, workspace=workspace)
+        check(x, u, k=rng.integers(1, V, rows), p=rng.random(rows), workspace=workspace)
+
+
+def test_a_share_outside():
+    """u below 0 and NaN take the first token, above 1 the last that is kept."""
+    rng = np.random.default_rng(5)
+    x = logits(rng, 4, 3000)
+    got, _ = draw(x, np.array([-1.0, np.nan, 2.0, np.inf]), k=np.full(4, 3))
+    order = np.argsort(-x, axis=1, kind="stable")
+    assert list(got) == [order[0, 0], order[1, 0], order[2, 2], order[3, 2]]
+
+
+def test_workspace_and_runs_change_nothing():
+    rng = np.random.default_rng(6)
+    rows, V = 64, 30000
+    x, u = logits(rng, rows, V), rng.random(rows)
+    kw = dict(T=rng.uniform(0.5, 1.5, rows), k=rng.choice([0, 40, 2000], rows), p=rng.choice([1, 0.9], rows))
+    first = draw(x, u, **kw)
+    for ws in (True, False, True):
+        got = draw(x, u, workspace=ws, **kw)
+        assert np.array_equal(first[0], got[0]) and np.array_equal(first[1], got[1])
+
+
+def test_shares_of_many_draws():
+    """Over evenly spaced u each token comes as often as its share says, within one."""
+    rng = np.random.default_rng(7)
+    n, V = 2048, 40
+    x = np.tile(logits(rng, 1, V, 1.0), (n, 1))
+    got, lp = draw(x, (np.arange(n) + 0.5) / n)
+    z = x[0].astype(np.float64)
+    w = np.exp(z - z.max())
+    share = w / w.sum()
+    assert np.abs(np.bincount(got, minlength=V) - n * share).max() <= 1 + 1e-6
+    assert np.abs(np.exp(lp.astype(np.float64)) - share[got]).max() <= 2.0 ** -22
+
+
+def test_many_rows_and_a_large_vocabulary():
+    rng = np.random.default_rng(8)
+    check(logits(rng, 300, 2000), rng.random(300), p=np.full(300, 0.9))
+    check(logits(rng, 2, 256000), rng.random(2), T=np.array([0.8, 1.5]), p=np.array([0.95, 1.0]))

@@ -1,0 +1,211 @@
+"""Without a GPU: refusals of the calls on a paged 8-bit KV cache and of the draw of
+tokens (nothing is launched for arguments that a kernel could not take), and pins
+of the plain definitions that the GPU tests compare with."""
+import numpy as np
+import pytest
+
+from oracle import pages8 as O
+from oracle.sample import sample
+from paper_2504_03664_amd import binding as B
+
+P = 1 << 20     # an address that no refused call touches
+
+
+def page(ps, h, d):
+    return 2 * ps * h * d + -(-ps * h // 2 // 128) * 128
+
+
+def cache(**kw):
+    base = dict(pool=P, layer_bytes=1 << 30, table=P, table_stride=8, n_layers=2, n_pages=100,
+                page_size=64, n_kv_heads=8, head_dim=128, n_seq=4, fmt=B.PIPO_KV8_E4M3)
+    base.update(kw)
+    return B.PipoKv8Pages(**base)
+
+
+def scores(**kw):
+    return B.PipoAttnScores(**kw)
+
+
+def status(fn, *args):
+    with pytest.raises(B.PipoError) as e:
+        fn(*args)
+    assert B.pipo_last_error() != ""
+    return B.STATUS_NAMES[e.value.status]
+
+
+def test_page_bytes():
+    assert B.pipo_kv8_page_bytes(64, 8, 128) == page(64, 8, 128) == 131072 + 256
+    assert B.pipo_kv8_page_bytes(16, 1, 64) == page(16, 1, 64) == 2048 + 128
+    for ps, h, d in ((8, 8, 128), (48, 8, 128), (512, 8, 128), (64, 0, 128), (64, 8, 96), (-64, 1, 64),
+                     (256, 1 << 16, 128)):
+        assert B.pipo_kv8_page_bytes(ps, h, d) == 0
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(pool=None), "PIPO_ERR_ARG"), (dict(table=None), "PIPO_ERR_ARG"), (dict(fmt=2), "PIPO_ERR_ARG"),
+    (dict(fmt=-1), "PIPO_ERR_ARG"), (dict(pool=P + 8), "PIPO_ERR_ARG"), (dict(n_pages=0), "PIPO_ERR_ARG"),
+    (dict(n_seq=0), "PIPO_ERR_ARG"), (dict(table_stride=0), "PIPO_ERR_ARG"),
+    (dict(layer_bytes=100 * page(64, 8, 128) - 16), "PIPO_ERR_ARG"),
+    (dict(layer_bytes=100 * page(64, 8, 128) + 8), "PIPO_ERR_ARG"),
+    (dict(n_layers=0), "PIPO_ERR_ARG"), (dict(page_size=24), "PIPO_ERR_UNSUPPORTED"),
+    (dict(head_dim=96), "PIPO_ERR_UNSUPPORTED"), (dict(n_kv_heads=0), "PIPO_ERR_UNSUPPORTED"),
+    (dict(n_seq=65536), "PIPO_ERR_UNSUPPORTED")])
+def test_bad_caches(kw, want):
+    c = cache(**kw)
+    assert status(B.pipo_op_kv8_pages_append, c, 0, P, P, P, 1024, P, 1024, 1) == want
+    assert status(B.pipo_op_kv8_pages_read, c, 0, P, P, P, 1024, P, 1024, 1) == want
+    assert status(B.pipo_op_attn_kv8_pages, c, 0, None, P, 4096, P, P, P, 4096, 32, 4, 1, 512) == want
+    assert status(B.pipo_op_kv8_pages_copy, c, P, P, 1) == want
+
+
+@pytest.mark.parametrize("layer", [-1, 2])
+def test_bad_layers(layer):
+    assert status(B.pipo_op_kv8_pages_append, cache(), layer, P, P, P, 1024, P, 1024,
+                  1) == "PIPO_ERR_ARG"
+    assert status(B.pipo_op_attn_kv8_pages, cache(), layer, None, P, 4096, P, P, P, 4096, 32, 4, 1,
+                  512) == "PIPO_ERR_ARG"
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(a=None), "PIPO_ERR_ARG"), (dict(b=None), "PIPO_ERR_ARG"), (dict(k=None), "PIPO_ERR_ARG"),
+    (dict(v=None), "PIPO_ERR_ARG"), (dict(ldk=1023), "PIPO_ERR_ARG"), (dict(ldv=0), "PIPO_ERR_ARG"),
+    (dict(M=-1), "PIPO_ERR_ARG"), (dict(M=1 << 31), "PIPO_ERR_UNSUPPORTED")])
+def test_bad_rows(kw, want):
+    a = dict(a=P, b=P, k=P, ldk=1024, v=P, ldv=1024, M=1)
+    a.update(kw)
+    assert status(B.pipo_op_kv8_pages_append, cache(), 0, *a.values()) == want
+    assert status(B.pipo_op_kv8_pages_read, cache(), 0, *a.values()) == want
+
+
+@pytest.mark.parametrize("args", [(None, P, 1), (P, None, 1), (P, P, -1)])
+def test_bad_copies(args):
+    assert status(B.pipo_op_kv8_pages_copy, cache(), *args) == "PIPO_ERR_ARG"
+
+
+def test_nothing_to_do():
+    B.pipo_op_kv8_pages_append(cache(), 0, P, P, P, 1024, P, 1024, 0)
+    B.pipo_op_kv8_pages_read(cache(), 0, P, P, P, 1024, P, 1024, 0)
+    B.pipo_op_kv8_pages_copy(cache(), P, P, 0)
+    B.pipo_op_attn_kv8_pages(cache(), 0, None, P, 4096, P, P, P, 4096, 32, 0, 1, 512)
+    B.pipo_op_attn_kv8_pages(cache(), 0, None, P, 4096, P, P, P, 4096, 32, 4, 0, 512)
+    B.pipo_op_sample(P, 10, None, None, None, None, P, P, None, 0, 10)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(q=None), "PIPO_ERR_ARG"), (dict(q_start=None), "PIPO_ERR_ARG"),
+    (dict(kv_len=None), "PIPO_ERR_ARG"), (dict(o=None), "PIPO_ERR_ARG"),
+    (dict(ldq=4095), "PIPO_ERR_ARG"), (dict(ldo=4095), "PIPO_ERR_ARG"),
+    (dict(n_heads=33), "PIPO_ERR_ARG"), (dict(n_heads=0), "PIPO_ERR_ARG"), (dict(M=-1), "PIPO_ERR_ARG"),
+    (dict(max_q=-1), "PIPO_ERR_ARG"), (dict(max_len=513), "PIPO_ERR_ARG"),
+    (dict(max_len=-1), "PIPO_ERR_ARG"), (dict(wsb=-1), "PIPO_ERR_ARG"),
+    (dict(f=scores(cap=-1.0)), "PIPO_ERR_ARG"), (dict(f=scores(cap=float("nan"))), "PIPO_ERR_ARG"),
+    (dict(f=scores(cap=float("inf"))), "PIPO_ERR_ARG"), (dict(f=scores(window=-1)), "PIPO_ERR_ARG"),
+    (dict(f=scores(max_prefix=-1)), "PIPO_ERR_ARG"),
+    (dict(M=1 << 26), "PIPO_ERR_UNSUPPORTED"), (dict(M=1 << 25, max_q=1 << 25), "PIPO_ERR_UNSUPPORTED"),
+    (dict(n_heads=65536, ldq=1 << 24, ldo=1 << 24), "PIPO_ERR_UNSUPPORTED")])
+def test_bad_attention(kw, want):
+    a = dict(f=None, q=P, ldq=4096, q_start=P, kv_len=P, o=P, ldo=4096, n_heads=32, M=4, max_q=1,
+             max_len=512, ws=None, wsb=0)
+    a.update(kw)
+    assert status(B.pipo_op_attn_kv8_pages, cache(), 0, *a.values()) == want
+
+
+def test_attention_workspace():
+    c = cache(n_seq=1, table_stride=1024, pool=None, table=None)
+    ws = B.pipo_op_attn_kv8_pages_workspace_bytes
+    n = ws(c, None, 32, 1, 1, 65536)
+    assert n > 0 and n % (32 * 130 * 4) == 0
+    assert ws(c, None, 33, 1, 1, 65536) == 0 and ws(c, None, 32, 0, 1, 65536) == 0
+    assert ws(c, scores(cap=-1.0), 32, 1, 1, 65536) == 0
+    assert ws(c, None, 32, 1, 1, 100) == 0                       # too short to split
+    assert ws(c, scores(window=128), 32, 1, 1, 65536) == 0       # and so is what is seen
+    many = cache(n_seq=4096, table_stride=1024, pool=None, table=None)
+    assert ws(many, None, 32, 4096, 1, 4096) == 0                # enough workgroups
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(logits=None), "PIPO_ERR_ARG"), (dict(u=None), "PIPO_ERR_ARG"), (dict(next=None), "PIPO_ERR_ARG"),
+    (dict(rows=-1), "PIPO_ERR_ARG"), (dict(V=0), "PIPO_ERR_ARG"), (dict(ld=99), "PIPO_ERR_ARG"),
+    (dict(wsb=-1), "PIPO_ERR_ARG"), (dict(V=(1 << 23) + 1, ld=1 << 24), "PIPO_ERR_UNSUPPORTED"),
+    (dict(rows=1 << 22), "PIPO_ERR_UNSUPPORTED")])
+def test_bad_sample(kw, want):
+    a = dict(logits=P, ld=100, T=None, k=None, p=None, m=None, u=P, next=P, logprob=None, rows=2, V=100,
+             ws=None, wsb=0)
+    a.update(kw)
+    assert status(B.pipo_op_sample, *a.values()) == want
+
+
+def test_sample_workspace():
+    assert B.pipo_op_sample_workspace_bytes(1, 1) > 0
+    assert B.pipo_op_sample_workspace_bytes(64, 128256) >= 64 * B.pipo_op_sample_workspace_bytes(1, 1)
+    for rows, V in ((0, 10), (1, 0), (-1, 10), (1, (1 << 23) + 1)):
+        assert B.pipo_op_sample_workspace_bytes(rows, V) == 0
+
+
+# ---------------------------------------------------------------------------
+def test_codes():
+    e4m3 = [m * 2.0 ** -9 for m in range(8)] + [(1 + m / 8) * 2.0 ** e for e in range(-6, 9)
+                                               for m in range(8)][:-1]
+    assert max(e4m3) == 448 and len(e4m3) == 127
+    for fmt, numbers in (("e4m3", e4m3), ("int8", [float(i) for i in range(128)])):
+        numbers = np.array(numbers)
+        assert np.array_equal(O.nearest(numbers, fmt), numbers)
+        mid = (numbers[1:] + numbers[:-1]) / 2
+        assert np.array_equal(O.nearest(mid * (1 + 1e-9), fmt), numbers[1:])
+        assert np.array_equal(O.nearest(-mid * (1 - 1e-9), fmt), -numbers[:-1])
+        even = np.where(np.arange(len(mid)) % 2 == 0, numbers[:-1], numbers[1:])
+        assert np.array_equal(O.nearest(mid, fmt), even)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_what_a_code_stands_for_is_a_half(fmt):
+    lo, hi = O.EXPONENTS[fmt]
+    x = O.nearest(np.linspace(-O.TOP[fmt], O.TOP[fmt], 4001), fmt)
+    for e in (lo, lo + 1, 0, hi):
+        y = x * 2.0 ** e
+        y = y[np.abs(y) <= O.CLAMP]
+        assert np.array_equal(y.astype(np.float16).astype(np.float64), y)
+    assert O.TOP[fmt] * 2.0 ** hi >= O.CLAMP
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_blocks(fmt):
+    rng = np.random.default_rng(1)
+    rows = rng.standard_normal((40, 2, 64)).astype(np.float16)
+    one, parts = O.Blocks(2, 64, fmt), O.Blocks(2, 64, fmt)
+    one.append(rows, 40)
+    step = (np.abs(rows).max() * (2.0 ** -4 if fmt == "e4m3" else 2.0 ** -7))
+    assert np.abs(one.values() - rows).max() <= step
+    for a, b in ((0, 3), (3, 4), (4, 20), (20, 40)):
+        parts.append(rows[a:b], b)
+    # the same scales in the end, and the codes where nothing grew
+    assert np.array_equal(one.exps, parts.exps)
+    assert np.abs(one.values() - parts.values()).max() <= 2 * step
+    parts.append(rows[:0], 5)
+    assert len(parts.values()) == 5
+
+
+def test_attention_definition():
+    rng = np.random.default_rng(2)
+    q, k, v = (rng.standard_normal((n, 1, 8)) for n in (3, 5, 5))
+    o = O.attention(q, k, v, cap=2.0, slopes=np.array([0.5]), window=2, prefix=1)
+    s = 2 * np.tanh(q[1, 0] @ k[:, 0].T / 2) - 0.5 * np.abs(3 - np.arange(5))
+    p = np.exp(s[[0, 2, 3]])
+    assert np.allclose(o[1, 0], p @ v[[0, 2, 3], 0] / p.sum())
+    assert np.array_equal(O.seen(3, 2), [[0, 0], [1, 0], [1, 1]])
+    assert (O.attention(q, k[:2], v[:2])[0] == 0).all()
+
+
+def test_sample_definition():
+    x = np.log(np.array([0.1, 0.4, 0.2, 0.3], np.float32))
+    order = [1, 3, 2, 0]
+    for u, want in ((0.0, 0), (0.39, 0), (0.41, 1), (0.69, 1), (0.71, 2), (0.89, 2), (0.91, 3), (1.0, 3)):
+        assert sample(x, u)[0] == order[want]
+    assert sample(x, 0.99, top_k=2)[0] == 3 and sample(x, 0.99, top_p=0.6)[0] == 3
+    assert sample(x, 0.99, top_p=0.3)[0] == 1 and sample(x, 0.99, min_p=0.45)[0] == 2
+    assert sample(x, 0.99, T=0.0) == (1, 0.0) and sample(x, 0.99, T=float("nan")) == (1, 0.0)
+    assert np.isclose(sample(x, 0.99, top_k=2)[1], np.log(0.3 / 0.7))
+    assert sample(np.full(3, np.nan), 0.5) == (0, -np.inf)
+    assert sample(np.array([np.nan, -np.inf, 1.0]), 0.5) == (2, 0.0)
+    assert sample(np.array([np.inf, 1.0, np.inf]), 0.9) == (2, np.log(0.5))
+    assert sample(np.ones(10), 0.35)[0] == 3 and sample(np.ones(10), 0.99, top_k=4)[0] == 3

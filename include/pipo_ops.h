@@ -505,12 +505,12 @@ int64_t pipo_op_argmax_workspace_bytes(int64_t rows, int64_t V);
  * T that is not above 0 (NaN too) takes the largest logit, with logprob 0.  NaN and -infinite
  * logits are never drawn; of infinite ones alone; a row with nothing else gives 0, and
  * logprob -infinity.  Weights under e^-31 of the largest count as none.  Weights are
- * held to 2^-36 of their size and summed as whole numbers, so the result does not depend
+ * held to 2^-31 of their size and summed as whole numbers, so the result does not depend
  * on the workspace or on the run.
  * workspace (device, caller-owned, contents arbitrary, 16-byte aligned) of
  * pipo_op_sample_workspace_bytes(rows, V) bytes lets several workgroups share a row; with less
  * (or NULL) one does it all: the same result.  Calls sharing a workspace must not overlap
- * in time.  V up to 2^23 and rows below 2^22, else PIPO_ERR_UNSUPPORTED.
+ * in time.  V up to 2^23 and rows below 2^21, else PIPO_ERR_UNSUPPORTED.
  */
 pipo_status pipo_op_sample(const float* logits, int64_t ld, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p,

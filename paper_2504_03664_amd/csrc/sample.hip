@@ -3,13 +3,17 @@
 // logits (equal ones by index), which top-k, min-p and top-p each cut to a prefix.
 //
 // So everything asked of a row is a place in that order, by rank or by running
-// weight.  With t = 8 x / T in 64 bits, a token is in bin floor(t), and its weight
-// is exp((b + 1/2) / 8) of its bin times exp of what is left of t / 8, at most
-// 1/16 away from 0, as a whole number of units 2^-36.  Bins are in order, the
-// order inside a bin is found only for the bins that hold a place asked for, and
-// sums of whole numbers do not depend on how a row is split or on atomics' order.
-// Bins more than 255 below the largest logit's, under e^-31 of its weight, count
-// as nothing.
+// weight.  With t = 8 x / T, rounded to 2^-32, a token is in bin floor(t), and its weight is
+// exp((b + 1/2) / 8) of its bin times exp of what is left of t / 8, at most 1/16 away
+// from 0, as a whole number of units 2^-36.  Bins are in order, the order inside a bin
+// is found only for the bins that hold a place asked for, and sums of whole numbers
+// do not depend on how a row is split or on atomics' order.  Bins more than 255 below
+// the largest logit's, under e^-31 of its weight, count as nothing.
+//
+//   sample_slices_k: a workgroup for each slice of a row: its bins, and the tokens of
+//                    the first of them.  One read of the logits, held in registers.
+//   sample_rows_k:   a workgroup for each row: bins of all slices, the cuts, the draw.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -22,9 +26,12 @@ constexpr int kBins = 256;
 constexpr int kUnitBits = 36;             // of a weight
 constexpr int kCountShift = 50;           // of a bin's count above its weight, in a slice
 constexpr int kSliceMax = 8192;           // logits of a slice, so that both fit 64 bits
-constexpr int kListMax = 256;             // tokens of a slice's largest bins that it lists
-constexpr int kSortMax = 512;             // tokens that are put in order at once
+constexpr int kListMax = 64;              // tokens of a slice's first bins that it lists, at most
+constexpr int kCands = 4096;              // listed tokens of a row
+constexpr int kRank = 128;                // tokens that are put in order at once
+constexpr int kMaxSlices = 1024;
 constexpr int64_t kMaxV = (int64_t)1 << 23;
+static_assert(kMaxSlices * (int64_t)kSliceMax >= kMaxV, "slices of the largest row");
 typedef unsigned long long u64;
 
 // what one slice of a row leaves for the row's workgroup: its largest logit (with
@@ -45,57 +52,78 @@ struct SampleArgs {
   int32_t* next;
   float* logprob;
   Slice* slices;   // [rows][n_slices]
-  int V, n_slices, slice;
-  bool vec;        // rows on 16 bytes
+  int V, n_slices, list_log2;   // (tokens that a slice lists at most)
 };
 
-// 8 / T of a row, 0 where the largest logit is taken
+// 8 / T of a row, below 0 where the largest logit is taken
 __device__ __forceinline__ double row_rate(const SampleArgs& a, int64_t row) {
   const float T = a.T ? a.T[row] : 1.f;
   return T > 0.f ? 8.0 / (double)T : -1.0;
 }
 
-// a logit's place: bin below that of the largest logit m (t of m: tm, its bin bm)
-// and weight.  m infinite: its equals alone count, one unit each.
-struct Place {
-  int r;       // kBins: none
-  double f;    // t - floor(t)
+// Added to a t up to 2^19, this leaves floor(t) + 2^19 in the low 20 bits of the
+// upper word, and the fraction, rounded to 2^-32, as the lower word.
+constexpr double kMagic = 0x1.8p20;
+constexpr double kMagicMost = 0x1p18;  // of t, where it is used
+
+// a logit's bin (whole numbers; above kMagicMost t is a multiple of 2^-34 at the finest,
+// and only equal logits are near each other) and the fraction of t in units of 2^-32
+struct Spot {
+  double b;
+  uint32_t f;
 };
-__device__ __forceinline__ Place place_of(float x, float m, double rate, double bm) {
-#pragma clang fp contract(off)  // (t - floor(t) of the rounded t: else it leaves 0 .. 1 for large t)
-  Place p;
-  const double t = (double)x * rate, b = __builtin_floor(t), d = bm - b;
-  p.r = d < (double)kBins ? (int)d : kBins;
-  p.f = t - b;
-  if (__builtin_isinf(m)) {
-    p.r = x == m ? 0 : kBins;
-    p.f = 0.5;
+__device__ __forceinline__ Spot spot_of(float x, double rate) {
+#pragma clang fp contract(off)
+  const double t = (double)x * rate, b = __builtin_floor(t);
+  if (__builtin_fabs(t) <= kMagicMost) {
+    const uint64_t s = __builtin_bit_cast(uint64_t, __builtin_fma((double)x, rate, kMagic));
+    return Spot{(double)((int)(s >> 32 & 0xFFFFF) - (1 << 19)), (uint32_t)s};
   }
-  if (x == -INFINITY) p.r = kBins;
-  return p;
+  if (__builtin_isinf(t) || __builtin_isnan(t)) return Spot{(double)x, 1u << 31};
+  return Spot{b, (uint32_t)((t - b) * 0x1p32)};
 }
-// exp((f - 1/2) / 8) 2^kUnitBits, rounded: the series to the sixth power, whose rest is
-// below 2^-40 of it
-__device__ __forceinline__ u64 units_of(double f) {
-  const double d = (f - 0.5) * 0.125;
-  constexpr double one = (double)(1ull << kUnitBits);
-  double e = one / 720.0;
-  e = __builtin_fma(e, d, one / 120.0);
-  e = __builtin_fma(e, d, one / 24.0);
-  e = __builtin_fma(e, d, one / 6.0);
-  e = __builtin_fma(e, d, one / 2.0);
-  e = __builtin_fma(e, d, one);
-  e = __builtin_fma(e, d, one);
-  return (u64)__builtin_bit_cast(uint64_t, e + 0x1p52) & ((1ull << 52) - 1);
+// how far a logit's bin is below that of the largest logit m (bin bm); kBins: not counted
+__device__ __forceinline__ int bin_below(const Spot& s, float x, float m, double bm) {
+  const double d = bm - s.b;
+  return x == m ? 0 : x > -INFINITY && d < (double)kBins ? (int)d : kBins;   // (NaN: not)
 }
-__device__ __forceinline__ double bin_of(float m, double rate) {
-  return __builtin_isinf(m) ? (double)m : __builtin_floor((double)m * rate);
+// The same from the two words of one sum, whose upper words differ as bins do; what is
+// not `on` is for numbers of which hardly two are in one bin.
+struct Fast {
+  bool on;
+  int top;
+  float low;
+  double rate;
+  __device__ __forceinline__ Fast(float m, double r, double bm) : rate(r) {
+    on = __builtin_fabs(bm) < kMagicMost - 1024.0 && rate > 0.0;
+    top = (int)(__builtin_bit_cast(uint64_t, __builtin_fma((double)m, rate, kMagic)) >> 32);
+    low = (float)((double)m - 300.0 / rate);   // (past the last bin)
+  }
+  // (not below kBins: not counted; NaN neither)
+  __device__ __forceinline__ uint32_t bin(float x, uint32_t& f) const {
+    const uint64_t s = __builtin_bit_cast(uint64_t, __builtin_fma((double)fmaxf(x, low), rate, kMagic));
+    f = (uint32_t)s;
+    return (uint32_t)(top - (int)(s >> 32));
+  }
+};
+// exp(d) 2^kUnitBits, d = (f / 2^32 - 1/2) / 8: 1 + d in whole numbers, d^2 / 2 .. d^5 / 120 in
+// fp32, of which the last step is 2^-33 of the weight, and what is left out 2^-33.5
+__device__ __forceinline__ u64 units_of(uint32_t f) {
+  const float d = (float)(int)(f - 0x80000000u) * 0x1p-35f;
+  float q = __builtin_fmaf(d, 1.f / 120.f, 1.f / 24.f);
+  q = __builtin_fmaf(q, d, 1.f / 6.f);
+  q = __builtin_fmaf(q, d, 0.5f);
+  q = q * (d * d) * 0x1p36f;
+  return (1ull << kUnitBits) - (1ull << 32) + ((u64)f << 1) + (uint32_t)q;
 }
 
-// keys that rise as logits fall (-0 as 0)
+// keys that rise as logits fall (-0 as 0), and back
 __device__ __forceinline__ uint32_t falling(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? b : ~(b | 0x80000000u);
+}
+__device__ __forceinline__ float logit(uint32_t d) {
+  return __uint_as_float(d & 0x80000000u ? d : ~d & 0x7FFFFFFFu);
 }
 
 template <int W>
@@ -121,72 +149,64 @@ __device__ __forceinline__ int block_min(int v, int (&lds)[W]) {
   return v;
 }
 
-__device__ __forceinline__ float valid(float x) { return x == x ? x : -INFINITY; }
-
-// four consecutive logits from i on (past the end: none)
-__device__ __forceinline__ f4 load4(const SampleArgs& a, const float* row, int i, int end) {
-  f4 x = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (a.vec && i + 4 <= end) {
-    x = *reinterpret_cast<const f4*>(row + i);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (i + j < end) x[j] = row[i + j];
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) x[j] = valid(x[j]);
-  return x;
-}
-
-// One slice of a row: the logits stay in registers.
+// One slice of a row.
 template <int E>
 __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
-  static_assert(256 * E <= kSliceMax, "a bin's count and weight fit a word");
-  __shared__ u64 bins[4][kBins];
+  static_assert(E <= 32 && 256 * E <= kSliceMax, "a bin's count and weight fit a word");
+  __shared__ u64 bins[kBins][4];  // (a copy for every fourth lane, side by side)
   __shared__ float red[4];
   __shared__ int redi[4], scan[4], n_list;
   const int tid = threadIdx.x, lane = tid & 63;
   const int64_t row = blockIdx.x / a.n_slices;
   const int s = blockIdx.x - (int)row * a.n_slices;
-  const int lo = s * 256 * E, end = min(a.V, lo + 256 * E);
+  const int lo = s * 256 * E, n = min(a.V - lo, 256 * E);
   Slice& out = a.slices[(int64_t)row * a.n_slices + s];
-  const float* x = a.logits + row * a.ld;
-  f4 v[E / 4];
+  const float* x = a.logits + row * a.ld + lo;
+  float v[E];
+  if (n == 256 * E) {
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i) v[i] = load4(a, x, lo + 4 * (256 * i + tid), end);
-  for (int i = tid; i < 4 * kBins; i += 256) (&bins[0][0])[i] = 0;
+    for (int e = 0; e < E; ++e) v[e] = x[256 * e + tid];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = 256 * e + tid < n ? x[256 * e + tid] : -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bins[tid][i] = 0;
+  const double rate = row_rate(a, row);
   float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = fmaxf(m, v[i][j]);
+  for (int e = 0; e < E; ++e) m = fmaxf(m, v[e]);   // (NaN: the other)
   m = block_max(m, red);
-  const double rate = row_rate(a, row);
   if (rate < 0.0 || m == -INFINITY) {
     int arg = INT_MAX;
 #pragma unroll
-    for (int i = 0; i < E / 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (v[i][j] == m) arg = min(arg, lo + 4 * (256 * i + tid) + j);
+    for (int e = E - 1; e >= 0; --e) arg = v[e] == m ? 256 * e + tid : arg;
     arg = block_min(arg, redi);
     if (tid == 0) {
       out.m = m;
-      out.arg = arg;
+      out.arg = arg == INT_MAX ? 0 : lo + arg;
     }
     return;
   }
-  const double bm = bin_of(m, rate);
+  const double bm = spot_of(m, rate).b;
+  const Fast fast(m, rate, bm);
+  if (fast.on) {
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const Place p = place_of(v[i][j], m, rate, bm);
-      if (p.r < kBins) atomicAdd(&bins[lane & 3][p.r], units_of(p.f) + (1ull << kCountShift));
+    for (int e = 0; e < E; ++e) {
+      uint32_t f;
+      const uint32_t r = fast.bin(v[e], f);
+      if (r < kBins) atomicAdd(&bins[r][lane & 3], units_of(f) + (1ull << kCountShift));
     }
+  } else {
+    for (int i = tid; i < n; i += 256) {
+      const Spot p = spot_of(x[i], rate);
+      const int r = bin_below(p, x[i], m, bm);
+      if (r < kBins) atomicAdd(&bins[r][lane & 3], units_of(p.f) + (1ull << kCountShift));
+    }
+  }
   if (tid == 0) n_list = 0;
   __syncthreads();
-  const u64 h = bins[0][tid] + bins[1][tid] + bins[2][tid] + bins[3][tid];
+  const u64 h = bins[tid][0] + bins[tid][1] + bins[tid][2] + bins[tid][3];
   out.bin[tid] = h;
   // whole bins, as many as the list takes
   int c = (int)(h >> kCountShift);
@@ -198,18 +218,41 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
   if (lane == 63) scan[tid >> 6] = c;
   __syncthreads();
   for (int w = 0; w < tid >> 6; ++w) c += scan[w];
-  const int fits = __popcll(__ballot(c <= kListMax));
+  const int fits = __popcll(__ballot(c <= 1 << a.list_log2));
   if (lane == 0) redi[tid >> 6] = fits;
   __syncthreads();
   const int list_bins = redi[0] + redi[1] + redi[2] + redi[3];
+  // Their tokens, in any order; a wave takes its places at once.
+  if (fast.on) {
+    const float least = (float)((bm - list_bins) / rate);   // (a bin more, for the rounding)
+    uint64_t marks[E];
+    int total = 0;
 #pragma unroll
-  for (int i = 0; i < E / 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (place_of(v[i][j], m, rate, bm).r < list_bins) {
-        const int at = atomicAdd(&n_list, 1);  // (in any order)
-        out.list[at] = make_float2(v[i][j], __int_as_float(lo + 4 * (256 * i + tid) + j));
+    for (int e = 0; e < E; ++e) {
+      marks[e] = __ballot(v[e] >= least);
+      if (marks[e]) {
+        uint32_t f;
+        marks[e] &= __ballot(fast.bin(v[e], f) < (uint32_t)list_bins);
+        total += __popcll(marks[e]);
       }
+    }
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&n_list, total);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (marks[e]) {
+        if (marks[e] >> lane & 1)
+          out.list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(marks[e] >> 32),
+                                                  __builtin_amdgcn_mbcnt_lo((uint32_t)marks[e], 0))] =
+              make_float2(v[e], __int_as_float(lo + 256 * e + tid));
+        at += __popcll(marks[e]);
+      }
+  } else {
+    for (int i = tid; i < n; i += 256)
+      if (bin_below(spot_of(x[i], rate), x[i], m, bm) < list_bins)
+        out.list[atomicAdd(&n_list, 1)] = make_float2(x[i], __int_as_float(lo + i));
+  }
   __syncthreads();
   if (tid == 0) {
     out.m = m;
@@ -219,24 +262,71 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
   }
 }
 
+// Eight waves, two a SIMD: much of a row's work is a chain of dependent 64-bit steps that every
+// wave does alike, and takes longer where more of them share a SIMD.  The code is kept
+// small, since most of it runs once and is fetched as it runs.
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
+constexpr int kHeld = 1024;     // tokens of one bin that a wave keeps at hand
+constexpr u64 kNone = ~0ull;    // in place of a token (its logit a NaN)
+static_assert(kRowThreads >= kBins, "a thread for each bin");
+
+// exp(-r / 8) 2^-kUnitBits, the weight of a unit of bin r over the first bin's middle, and
+// its reciprocal
+struct Factors {
+  double of[kBins] = {}, per[kBins] = {};
+  constexpr Factors() {
+    double down = 1.0 / (double)(1ull << kUnitBits), up = (double)(1ull << kUnitBits);
+    for (int r = 0; r < kBins; ++r) {
+      of[r] = down;
+      per[r] = up;
+      down *= 0.88249690258459540;   // exp(-1/8)
+      up *= 1.1331484530668263;      // exp(1/8)
+    }
+  }
+};
+__constant__ const Factors kFactors = Factors();
 
 struct RowLds {
-  double cum_w[kBins];             // weights of the bins up to each
-  double factor[kBins];            // of a unit
-  u64 w[kBins], cum_c[kBins];      // a bin's units; counts up to each
-  u64 sub_w[kBins], sub_c[kBins];  // of parts of a bin
-  u64 key[kSortMax], unit[kSortMax];
+  double cum_w[kBins];               // weights of the bins up to each
+  double factor[kBins], per[kBins];  // of kFactors
+  u64 w[kBins], cum_c[kBins];        // a bin's units; counts up to each
   u64 bins_c[kBins];
+  u64 sub_w[kBins], sub_c[kBins];    // of parts of a bin
+  u64 key[kRank], unit[kRank];
   u64 part[kRowWaves];
   double dpart[kRowWaves];
+  u64 cand[kCands];                  // (key, index) of listed tokens, by bin
+  u64 held[kRowWaves][kHeld];        // of one bin's, or of a piece of the row
+  uint32_t info[kMaxSlices];         // a slice's bins below the row's, listed bins and tokens
   float red[kRowWaves];
-  int redi[kRowWaves];
-  int n, pick;
-  uint32_t lo, hi;
+  int redi[kRowWaves], firsts[kRowWaves];
+  uint32_t los[kRowWaves], his[kRowWaves];
+  int n, covered, pick, over;
 };
 
-// inclusive sums over kBins values, one for each of the first kBins threads
+// the first thread that has it (`none`: none has); no atomics, which go lane by lane
+__device__ __forceinline__ int first_of(bool has, int none, RowLds& lds) {
+  const uint64_t who = __ballot(has);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0)
+    lds.firsts[wave] = who ? 64 * wave + __ffsll((unsigned long long)who) - 1 : none;
+  __syncthreads();
+  int t = lds.firsts[0];
+#pragma unroll
+  for (int w = 1; w < kRowWaves; ++w) t = min(t, lds.firsts[w]);
+  __syncthreads();
+  return t;
+}
+// a place in lds.n for each lane that is here
+__device__ __forceinline__ int place_for(RowLds& lds) {
+  const uint64_t who = __ballot(true);
+  const int mine = __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+  int at = 0;
+  if (mine == 0) at = atomicAdd(&lds.n, (int)__popcll(who));
+  return __builtin_amdgcn_readfirstlane(at) + mine;
+}
+
+// inclusive sums over the first kBins threads' values
 template <typename T>
 __device__ __forceinline__ T scan_bins(T v, T (&part)[kRowWaves]) {
   const int tid = threadIdx.x, lane = tid & 63;
@@ -247,56 +337,175 @@ __device__ __forceinline__ T scan_bins(T v, T (&part)[kRowWaves]) {
   }
   if (lane == 63) part[tid >> 6] = v;
   __syncthreads();
-  for (int w = 0; w < tid >> 6 && w < kBins / 64; ++w) v += part[w];
+  for (int w = 0; w < tid >> 6; ++w) v += part[w];
   __syncthreads();
   return v;
 }
 
-// A row: SOLO without slices.
-template <bool SOLO>
+// Where a place is looked for: at a rank (from 1) or where the units so far are above the
+// target, or reach it; rank `most` at the latest.
+struct Ask {
+  bool by_rank, reach;
+  double target;
+  int64_t most;
+  __device__ __forceinline__ bool passes(u64 c, u64 w) const {
+    const double y = by_rank ? (double)c : (double)w;
+    return (int64_t)c >= most || (reach ? y >= target : y > target);
+  }
+};
+
 struct Row {
   const SampleArgs& a;
   RowLds& lds;
   const float* x;
-  const Slice* slices;
   float m;
-  double rate, bm, inv_T;
+  double rate, bm;
+  Fast fast;
+  // where the tokens asked for are: this thread's are entries `from`, `from` + `step` .. of
+  // the `count` at `at`, or (null) the logits, which each wave then takes through its part of
+  // `held`
+  const u64* at = nullptr;
+  int count = 0, from = 0, step = 64;
+  int held_bin = -1, n_held = 0;   // whose tokens are in `held`, how many of this wave's
 
-  // fn(logit, index) for every token of bin r
+  // this wave's piece i of the row into its part of `held`
+  __device__ __forceinline__ void stage(int i) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lo = (i * kRowWaves + wave) * kHeld;
+    constexpr int N = 16;
+#pragma unroll 1
+    for (int j = lane; j < kHeld; j += 64 * N) {
+      float y[N];
+#pragma unroll
+      for (int n = 0; n < N; ++n) y[n] = x[min(lo + j + 64 * n, a.V - 1)];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int i = lo + j + 64 * n;
+        lds.held[wave][j + 64 * n] =
+            i < a.V && y[n] > -INFINITY ? (u64)falling(y[n]) << 32 | (uint32_t)i : kNone;
+      }
+    }
+    held_bin = -1;
+  }
+  __device__ __forceinline__ int bin_of(float y, uint32_t& f) const {
+    if (fast.on) return (int)min(fast.bin(y, f), (uint32_t)kBins);
+    const Spot s = spot_of(y, rate);
+    f = s.f;
+    return bin_below(s, y, m, bm);
+  }
+  // fn(key, index, bin, fraction) for every token of the source
   template <typename F>
-  __device__ __forceinline__ void each(int r, F fn) const {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const auto test = [&](float v, int i) {
-      if (place_of(v, m, rate, bm).r == r) fn(v, i);
+  __device__ __forceinline__ void each(F fn) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int pieces = at ? 1 : (a.V + kRowWaves * kHeld - 1) / (kRowWaves * kHeld);
+    for (int i = 0; i < pieces; ++i) {
+      if (!at) stage(i);
+      const u64* e = at ? at : lds.held[wave];
+      const int n = at ? count : kHeld, j1 = at ? step : 64;
+#pragma unroll 1
+      for (int j = at ? from : lane; j < n; j += j1) {
+        const float y = logit((uint32_t)(e[j] >> 32));
+        uint32_t f;
+        const int b = bin_of(y, f);
+        fn((uint32_t)(e[j] >> 32), (int)(uint32_t)e[j], b, f);
+      }
+    }
+  }
+  // Makes the source the tokens of bin r whose t are `part` (in bins) or less from `from_top`
+  // below the bin's upper end, by wave; whether they fit.  Some beside them come along: as
+  // floats, ends and middle are rounded.
+  __device__ __forceinline__ bool hold(int r, double from_top, double part) {
+    constexpr int N = 8;   // 64 KiB asked for at a time, twice: a row comes from afar
+    const float mid = (float)((bm - r + 1.0 - from_top) / rate);
+    const float half = (float)((part + __builtin_fabs(bm) * 0x1p-21 + 0x1p-20) / rate);
+    held_bin = -1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    u64* out = lds.held[wave];
+    int n = 0;
+    const auto take = [&](float y, int i) {
+      const uint64_t hit = __ballot(__builtin_fabsf(y - mid) <= half);
+      if (hit) {
+        const int p = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
+                                                    __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
+        if ((hit >> lane & 1) && p < kHeld) out[p] = (uint32_t)i;
+        n += __popcll(hit);
+      }
     };
-    if constexpr (SOLO) {
-      for (int i = 4 * tid; i < a.V; i += 4 * kRowThreads) {
-        const f4 v = load4(a, x, i, a.V);
+    // up to the first 16-byte boundary, from there by four, and the rest
+    const int head = min((int)(-(reinterpret_cast<uintptr_t>(x) >> 2) & 3), a.V);
+    int i0 = head;
+    f4 v[2][N];
+    const auto ask = [&](f4(&y)[N], int i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) test(v[j], i + j);
-      }
-    } else {
-      for (int s = wave; s < a.n_slices; s += kRowWaves) {
-        const Slice& sl = slices[s];
-        if (sl.m == -INFINITY) continue;
-        const double off = sl.m == m ? 0.0 : bm - bin_of(sl.m, rate);
-        if (!(off <= (double)r)) continue;
-        const int at = r - (int)off;
-        if (sl.bin[at] >> kCountShift == 0) continue;
-        if (at < sl.list_bins) {
-          for (int i = lane; i < sl.n_list; i += 64) {
-            const float2 y = sl.list[i];
-            test(y.x, __float_as_int(y.y));
-          }
-        } else {
-          const int lo = s * a.slice, end = min(a.V, lo + a.slice);
-          for (int i = lo + 4 * lane; i < end; i += 256) {
-            const f4 v = load4(a, x, i, end);
+      for (int j = 0; j < N; ++j) y[j] = *reinterpret_cast<const f4*>(x + i + 4 * (j * kRowThreads + tid));
+    };
+    const auto sift = [&](const f4(&y)[N], int i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) test(v[j], i + j);
-          }
-        }
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) take(y[j][e], i + 4 * (j * kRowThreads + tid) + e);
+    };
+    constexpr int kPiece = 4 * N * kRowThreads;
+    if (i0 + kPiece <= a.V) ask(v[0], i0);
+#pragma unroll 1
+    while (i0 + kPiece <= a.V) {
+      if (i0 + 2 * kPiece <= a.V) ask(v[1], i0 + kPiece);
+      sift(v[0], i0);
+      i0 += kPiece;
+      if (i0 + kPiece > a.V) break;
+      if (i0 + 2 * kPiece <= a.V) ask(v[0], i0 + kPiece);
+      sift(v[1], i0);
+      i0 += kPiece;
+    }
+    constexpr int T = 16;
+    for (int i1 = i0 - head; i1 < a.V; i1 += T * kRowThreads) {
+      float v[T];
+#pragma unroll
+      for (int j = 0; j < T; ++j) v[j] = x[min(i1 + head + j * kRowThreads + tid, a.V - 1)];
+#pragma unroll
+      for (int j = 0; j < T; ++j) {
+        const int i = i1 + head + j * kRowThreads + tid;
+        take(i < a.V ? v[j] : NAN, i);
       }
+    }
+    if (wave == 0) take(tid < head ? x[min(tid, a.V - 1)] : NAN, tid);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (other lanes' entries)
+    __builtin_amdgcn_wave_barrier();
+    const bool over = n > kHeld;
+    n_held = min(n, kHeld);
+#pragma unroll 4
+    for (int j = lane; j < n_held; j += 64) {
+      const int i = (int)(uint32_t)out[j];
+      out[j] = (u64)falling(x[i]) << 32 | (uint32_t)i;
+    }
+    if (tid == 0) lds.over = 0;
+    __syncthreads();
+    if (over) lds.over = 1;
+    __syncthreads();
+    at = out;
+    count = n_held;
+    from = lane;
+    step = 64;
+    return !lds.over;
+  }
+  // the source for bin r, or for part `sub` of 256 of it (-1: all)
+  __device__ __forceinline__ void look_at(int r, int sub, int64_t n) {
+    at = nullptr;
+    if (r < lds.covered) {
+      at = lds.cand + (r > 0 ? lds.cum_c[r - 1] : 0);
+      count = (int)lds.bins_c[r];
+      from = threadIdx.x;
+      step = kRowThreads;
+    } else if (r == held_bin) {
+      at = lds.held[threadIdx.x >> 6];
+      count = n_held;
+      from = threadIdx.x & 63;
+      step = 64;
+    } else if (n <= kRowWaves * kHeld && fast.on) {
+      if (!hold(r, sub < 0 ? 0.5 : (sub + 0.5) / 256.0, sub < 0 ? 0.5 : 0.5 / 256.0))
+        at = nullptr;
+      else if (sub < 0)
+        held_bin = r;
     }
   }
 
@@ -304,95 +513,144 @@ struct Row {
     int64_t rank;   // in the bin, from 1
     double units;   // up to and with it
     float x;
-    int index;      // (of a pick that asks for it)
+    int index;
   };
-  // The token of bin r at a rank (by_rank: target, from 1), or the first one with which
-  // the units so far are above the target, or reach it (reach); rank `most` at the
-  // latest.
-  __device__ Pick pick(int r, bool by_rank, bool reach, double target, int64_t most, bool index) {
+  // the first of kBins parts (sub_c, sub_w) that holds the place; what is before it
+  // is added to c0 and w0, and its count returned in n
+  __device__ __forceinline__ int part_of(const Ask& q, u64& c0, u64& w0, int64_t& n) {
+    const int tid = threadIdx.x;
+    __syncthreads();
+    const u64 c = tid < kBins ? lds.sub_c[tid] : 0, w = tid < kBins ? lds.sub_w[tid] : 0;
+    const u64 cc = c0 + scan_bins(c, lds.part), cw = w0 + scan_bins(w, lds.part);
+    const int part = first_of(c > 0 && q.passes(cc, cw), kBins - 1, lds);
+    if (tid == part) {
+      lds.part[0] = cc - c;
+      lds.part[1] = cw - w;
+      lds.part[2] = c;
+    }
+    __syncthreads();
+    c0 = lds.part[0];
+    w0 = lds.part[1];
+    n = (int64_t)lds.part[2];
+    __syncthreads();
+    return part;
+  }
+
+  // The token of bin r that q asks for; with `weigh` the last one whose weight is at least
+  // exp(edge), and no rank if the bin has no fewer of them than q.most.
+  __device__ __forceinline__ Pick pick(int r, Ask q, bool weigh, double edge) {
     const int tid = threadIdx.x;
     int64_t n = lds.bins_c[r];
-    u64 c0 = 0, w0 = 0;   // before the part [lo, hi] of keys
+    u64 c0 = 0, w0 = 0;
+    // While they are many: by the fraction's first eight bits, then by keys from the least
+    // to the largest there are.
+    int sub = -1;
     uint32_t lo = 0, hi = 0xFFFFFFFFu;
-    if (n > kSortMax) {
-      if (tid == 0) {
-        lds.lo = 0xFFFFFFFFu;
-        lds.hi = 0;
-      }
-      __syncthreads();
-      each(r, [&](float v, int) {
-        atomicMin(&lds.lo, falling(v));
-        atomicMax(&lds.hi, falling(v));
-      });
-      __syncthreads();
-      lo = lds.lo;
-      hi = lds.hi;
-      while (n > kSortMax && lo != hi) {
-        const int shift = max(0, 32 - __clz(hi - lo) - 8);
-        if (tid < kBins) lds.sub_w[tid] = lds.sub_c[tid] = 0;
+    const auto mine = [&](uint32_t d, int b, uint32_t f) {
+      return b == r && d >= lo && d <= hi && (sub < 0 || (int)(~f >> 24) == sub);
+    };
+#pragma unroll 1
+    do {
+      look_at(r, sub, n);
+      if (weigh) {
+        weigh = false;
+        if (tid == 0) lds.n = 0;
         __syncthreads();
-        each(r, [&](float v, int) {
-          const uint32_t d = falling(v);
-          if (d < lo || d > hi) return;
-          atomicAdd(&lds.sub_c[(d - lo) >> shift], 1ull);
-          atomicAdd(&lds.sub_w[(d - lo) >> shift], units_of(place_of(v, m, rate, bm).f));
+        each([&](uint32_t d, int, int b, uint32_t) {
+          if (b == r && ((double)logit(d) - (double)m) * (rate * 0.125) >= edge) place_for(lds);
         });
         __syncthreads();
-        const u64 c = tid < kBins ? lds.sub_c[tid] : 0, w = tid < kBins ? lds.sub_w[tid] : 0;
-        const u64 cc = c0 + scan_bins(c, lds.part), cw = w0 + scan_bins(w, lds.part);
-        if (tid == 0) lds.pick = kBins;
+        const int64_t keep = lds.n;
         __syncthreads();
-        // the first part that holds the place, or the last allowed rank
-        if (tid < kBins && c > 0 && passes(cc, cw, by_rank, reach, target, most)) atomicMin(&lds.pick, tid);
-        __syncthreads();
-        const int q = min(lds.pick, kBins - 1);   // (one passes: most is at most n)
-        if (tid == q) {
-          lds.part[0] = cc - c;
-          lds.part[1] = cw - w;
-          lds.part[2] = c;
-        }
-        __syncthreads();
-        c0 = lds.part[0];
-        w0 = lds.part[1];
-        n = (int64_t)lds.part[2];
-        __syncthreads();
-        lo += (uint32_t)q << shift;
-        hi = min(hi, lo + ((1u << shift) - 1));
+        Pick p{keep, 0.0, 0.f, 0};
+        if (keep >= q.most) p.rank = -1;
+        if (keep >= q.most || keep == 0) return p;
+        q.target = (double)keep;
+        q.most = keep;
       }
+      if (n <= kRank || sub >= 0) break;
+      if (tid < kBins) lds.sub_w[tid] = lds.sub_c[tid] = 0;
+      __syncthreads();
+      each([&](uint32_t d, int, int b, uint32_t f) {
+        if (b != r) return;
+        atomicAdd(&lds.sub_c[~f >> 24], 1ull);
+        atomicAdd(&lds.sub_w[~f >> 24], units_of(f));
+      });
+      sub = part_of(q, c0, w0, n);
+    } while (!at);
+#pragma unroll 1
+    while (n > kRank && lo < hi) {
+      uint32_t least = 0xFFFFFFFFu, most = 0;
+      each([&](uint32_t d, int, int b, uint32_t f) {
+        if (!mine(d, b, f)) return;
+        least = min(least, d);
+        most = max(most, d);
+      });
+#pragma unroll
+      for (int k = 1; k < 64; k *= 2) {
+        least = min(least, (uint32_t)__shfl_xor((int)least, k, 64));
+        most = max(most, (uint32_t)__shfl_xor((int)most, k, 64));
+      }
+      if ((tid & 63) == 0) {
+        lds.los[tid >> 6] = least;
+        lds.his[tid >> 6] = most;
+      }
+      __syncthreads();
+      lo = lds.los[0];
+      hi = lds.his[0];
+#pragma unroll
+      for (int k = 1; k < kRowWaves; ++k) {
+        lo = min(lo, lds.los[k]);
+        hi = max(hi, lds.his[k]);
+      }
+      __syncthreads();
+      if (lo >= hi) break;
+      const int shift = max(0, 32 - __clz(hi - lo) - 8);
+      if (tid < kBins) lds.sub_w[tid] = lds.sub_c[tid] = 0;
+      __syncthreads();
+      each([&](uint32_t d, int, int b, uint32_t f) {
+        if (!mine(d, b, f)) return;
+        atomicAdd(&lds.sub_c[(d - lo) >> shift], 1ull);
+        atomicAdd(&lds.sub_w[(d - lo) >> shift], units_of(f));
+      });
+      lo += (uint32_t)part_of(q, c0, w0, n) << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
     }
-    if (n > kSortMax) return pick_equal(r, lo, n, c0, w0, by_rank, reach, target, most, index);
+    if (n > kRank) return pick_equal(lo, n, c0, w0, q);
     // in order: every token finds its place among the others
-    if (tid == 0) {
-      lds.n = 0;
-      lds.pick = INT_MAX;
-    }
+    if (tid == 0) lds.n = 0;
     __syncthreads();
-    each(r, [&](float v, int i) {
-      const uint32_t d = falling(v);
-      if (d < lo || d > hi) return;
-      const int at = atomicAdd(&lds.n, 1);
-      if (at >= kSortMax) return;
-      lds.key[at] = (u64)d << 32 | (uint32_t)i;
-      lds.unit[at] = units_of(place_of(v, m, rate, bm).f);
+    each([&](uint32_t d, int i, int b, uint32_t f) {
+      if (!mine(d, b, f)) return;
+      const int p = place_for(lds);
+      if (p >= kRank) return;
+      lds.key[p] = (u64)d << 32 | (uint32_t)i;
+      lds.unit[p] = units_of(f);
     });
     __syncthreads();
-    n = min(lds.n, kSortMax);
-    u64 mine = 0, c = c0, w = w0;
+    n = min(lds.n, kRank);
+    u64 key = 0, c = c0, w = w0;
     if (tid < n) {
-      mine = lds.key[tid];
+      key = lds.key[tid];
+#pragma unroll 4
       for (int j = 0; j < n; ++j) {
-        const bool before = lds.key[j] <= mine;
+        const bool before = lds.key[j] <= key;
         c += before;
         w += before ? lds.unit[j] : 0;
       }
-      if (passes(c, w, by_rank, reach, target, most)) atomicMin(&lds.pick, (int)(c - c0));
     }
+    // of those that pass the one with the fewest before it, or the last of all
+    int rank = tid < n && q.passes(c, w) ? (int)(c - c0) : (int)n;
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) rank = min(rank, __shfl_xor(rank, k, 64));
+    if ((tid & 63) == 0) lds.redi[tid >> 6] = rank;
     __syncthreads();
-    const int64_t rank = min((int64_t)lds.pick, n);
-    if (tid < n && (int64_t)(c - c0) == rank) {
+#pragma unroll
+    for (int k = 0; k < kRowWaves; ++k) rank = min(rank, lds.redi[k]);
+    if (tid < n && (int)(c - c0) == rank) {
       lds.part[0] = c;
       lds.part[1] = w;
-      lds.part[2] = mine;
+      lds.part[2] = key;
     }
     __syncthreads();
     Pick p;
@@ -403,25 +661,15 @@ struct Row {
     __syncthreads();
     return p;
   }
-  static __device__ __forceinline__ bool passes(u64 c, u64 w, bool by_rank, bool reach, double target,
-                                                int64_t most) {
-    if ((int64_t)c >= most) return true;
-    return by_rank ? (double)c >= target : reach ? (double)w >= target : (double)w > target;
-  }
-  static __device__ __forceinline__ float logit(uint32_t d) {  // of falling()
-    return __uint_as_float(d & 0x80000000u ? d : ~d & 0x7FFFFFFFu);
-  }
-  // among more equal tokens than fit: their weights are equal, so the rank is a quotient,
-  // and the index is found by counting
-  __device__ Pick pick_equal(int r, uint32_t d, int64_t n, u64 c0, u64 w0, bool by_rank, bool reach,
-                             double target, int64_t most, bool index) {
+  // among more equal tokens than fit: their weights are equal, so the rank is found by
+  // halving, and the index by counting
+  __device__ __forceinline__ Pick pick_equal(uint32_t d, int64_t n, u64 c0, u64 w0, const Ask& q) {
     const float v = logit(d);
-    const u64 unit = units_of(place_of(v, m, rate, bm).f);
-    // the least rank from 1 that passes, by halving
+    const u64 unit = units_of(spot_of(v, rate).f);
     int64_t lo = 1, hi = n;
     while (lo < hi) {
       const int64_t mid = (lo + hi) / 2;
-      if (passes(c0 + mid, w0 + mid * unit, by_rank, reach, target, most))
+      if (q.passes(c0 + mid, w0 + mid * unit))
         hi = mid;
       else
         lo = mid + 1;
@@ -431,15 +679,17 @@ struct Row {
     p.units = (double)(w0 + lo * unit);
     p.x = v;
     p.index = 0;
-    if (!index) return p;
     const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int N = 16;   // neighbours of a thread
     int64_t before = 0;
-    for (int i0 = 0; i0 < a.V; i0 += 4 * kRowThreads) {
-      const f4 y = load4(a, x, i0 + 4 * tid, a.V);
-      int c = 0;
+    for (int i0 = 0; i0 < a.V; i0 += N * kRowThreads) {
+      uint32_t marks = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c += y[j] == v;
-      int run = c;
+      for (int j = 0; j < N; ++j) {
+        const int i = i0 + N * tid + j;
+        if (i < a.V) marks |= (uint32_t)(x[i] == v) << j;
+      }
+      int run = __popc(marks);
 #pragma unroll
       for (int k = 1; k < 64; k *= 2) {
         const int z = __shfl_up(run, k, 64);
@@ -453,9 +703,9 @@ struct Row {
         total += lds.redi[w];
       }
       if (before + total >= lo) {   // here: the thread that has it says which
-        int64_t at = before + run - c;
-        for (int j = 0; j < 4; ++j)
-          if (y[j] == v && ++at == lo) lds.pick = i0 + 4 * tid + j;
+        int64_t has = before + run - __popc(marks);
+        for (; marks && has + 1 < lo; ++has) marks &= marks - 1;
+        if (marks && has + 1 == lo) lds.pick = i0 + N * tid + __ffs(marks) - 1;
         __syncthreads();
         p.index = lds.pick;
         __syncthreads();
@@ -468,37 +718,56 @@ struct Row {
   }
 };
 
+// SOLO: without slices.
 template <bool SOLO>
 __global__ __launch_bounds__(kRowThreads) void sample_rows_k(SampleArgs a) {
   __shared__ RowLds lds;
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
-  Row<SOLO> R{a, lds, a.logits + row * a.ld, a.slices + row * a.n_slices, -INFINITY, 0.0, 0.0, 0.0};
-  R.rate = row_rate(a, row);
+  const Slice* slices = a.slices + row * a.n_slices;
+  const double rate = row_rate(a, row);
+  const float* x = a.logits + row * a.ld;
+  const int64_t top_k = a.k ? a.k[row] : 0;
+  const float min_p = a.min_p ? a.min_p[row] : 0.f, top_p = a.p ? a.p[row] : 1.f, u = a.u[row];
+  const double factor = kFactors.of[tid & (kBins - 1)], per = kFactors.per[tid & (kBins - 1)];
+  // What the slices left, asked for at once (it was written far away a moment ago): 32
+  // slices' bins and 16 slices' lists, the others' below.
+  constexpr int kAhead = 32, kListed = 2;
+  static_assert(kAhead * kBins <= kRowWaves * kHeld && kRowThreads == 2 * kBins, "bins by way of `held`");
+  u64 ahead[kAhead / 2];
+  float2 listed[kListed];
+  Slice const* const last = slices + a.n_slices - 1;
+  float4 head = make_float4(-INFINITY, 0.f, 0.f, 0.f);
   float m = -INFINITY;
   if constexpr (SOLO) {
-    for (int i = 4 * tid; i < a.V; i += 4 * kRowThreads) {
-      const f4 v = load4(a, R.x, i, a.V);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) m = fmaxf(m, v[j]);
-    }
+#pragma unroll 8
+    for (int i = tid; i < a.V; i += kRowThreads) m = fmaxf(m, x[i]);
   } else {
-    for (int s = tid; s < a.n_slices; s += kRowThreads) m = fmaxf(m, R.slices[s].m);
+    head = *reinterpret_cast<const float4*>(min(slices + tid, last));
+#pragma unroll
+    for (int j = 0; j < kAhead / 2; ++j)
+      ahead[j] = min(slices + 2 * j + tid / kBins, last)->bin[tid & (kBins - 1)];
+#pragma unroll
+    for (int j = 0; j < kListed; ++j) {
+      const int e = j * kRowThreads + tid;
+      listed[j] = min(slices + (e >> a.list_log2), last)->list[e & ((1 << a.list_log2) - 1)];
+    }
+    m = head.x;
+    for (int s = tid + kRowThreads; s < a.n_slices; s += kRowThreads) m = fmaxf(m, slices[s].m);
   }
+  if (tid < kBins) lds.w[tid] = lds.bins_c[tid] = 0;
+  if (tid == 0) lds.covered = SOLO ? 0 : kBins;
   m = block_max(m, lds.red);
-  if (R.rate < 0.0 || m == -INFINITY) {   // the largest; nothing to draw from: 0
+  if (rate < 0.0 || m == -INFINITY) {   // the largest; nothing to draw from: 0
     int arg = INT_MAX;
     if (m != -INFINITY) {
       if constexpr (SOLO) {
-        for (int i = 4 * tid; i < a.V; i += 4 * kRowThreads) {
-          const f4 v = load4(a, R.x, i, a.V);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (v[j] == m) arg = min(arg, i + j);
-        }
+#pragma unroll 4
+        for (int i = tid; i < a.V; i += kRowThreads)
+          if (x[i] == m) arg = min(arg, i);
       } else {
         for (int s = tid; s < a.n_slices; s += kRowThreads)
-          if (R.slices[s].m == m) arg = min(arg, R.slices[s].arg);
+          if (slices[s].m == m) arg = min(arg, slices[s].arg);
       }
     }
     arg = block_min(arg, lds.redi);
@@ -508,55 +777,95 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_k(SampleArgs a) {
     }
     return;
   }
-  R.m = m;
-  R.bm = bin_of(m, R.rate);
-  R.inv_T = R.rate * 0.125;
+  const double bm = spot_of(m, rate).b, inv_T = rate * 0.125;
+  Row R{a, lds, x, m, rate, bm, Fast(m, rate, bm)};
 
-  // bins of the row
-  if (tid < kBins) lds.w[tid] = lds.bins_c[tid] = 0;
-  __syncthreads();
+  // bins of the row, and the tokens that its slices list
+  u64 w = 0, c = 0;
   if constexpr (SOLO) {
-    for (int i = 4 * tid; i < a.V; i += 4 * kRowThreads) {
-      const f4 v = load4(a, R.x, i, a.V);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const Place p = place_of(v[j], m, R.rate, R.bm);
-        if (p.r < kBins) {
-          atomicAdd(&lds.w[p.r], units_of(p.f));
-          atomicAdd(&lds.bins_c[p.r], 1ull);
-        }
-      }
+    R.each([&](uint32_t, int, int b, uint32_t f) {
+      if (b >= kBins) return;
+      atomicAdd(&lds.w[b], units_of(f));
+      atomicAdd(&lds.bins_c[b], 1ull);
+    });
+    __syncthreads();
+    if (tid < kBins) {
+      w = lds.w[tid];
+      c = lds.bins_c[tid];
     }
   } else {
-    const int r = tid & (kBins - 1);
-    u64 w = 0, c = 0;
-    for (int s = tid / kBins; s < a.n_slices; s += kRowThreads / kBins) {
-      const float ms = R.slices[s].m;
-      if (ms == -INFINITY) continue;
-      const double off = ms == m ? 0.0 : R.bm - bin_of(ms, R.rate);
-      if (!(off <= (double)r)) continue;
-      const u64 h = R.slices[s].bin[r - (int)off];
-      w += h & ((1ull << kCountShift) - 1);
-      c += h >> kCountShift;
+    for (int s = tid; s < a.n_slices; s += kRowThreads) {
+      if (s != tid) head = *reinterpret_cast<const float4*>(slices + s);
+      const int n_list = __float_as_int(head.z), list_bins = __float_as_int(head.w);
+      double off = kBins;
+      if (head.x != -INFINITY) off = head.x == m ? 0.0 : bm - spot_of(head.x, rate).b;
+      uint32_t info = kBins;   // nothing of it counts
+      if (off < (double)kBins) {
+        info = (uint32_t)(int)off | (uint32_t)list_bins << 9 | (uint32_t)n_list << 18;
+        atomicMin(&lds.covered, (int)off + list_bins);
+      }
+      lds.info[s] = info;
     }
-    atomicAdd(&lds.w[r], w);
-    atomicAdd(&lds.bins_c[r], c);
+    __syncthreads();
+    // a slice's bins into the row's, as far below as its largest logit is: kAhead slices at a
+    // time, by way of LDS, where a thread finds what is its bin's
+    u64(*const all)[kBins] = reinterpret_cast<u64(*)[kBins]>(&lds.held[0][0]);
+    for (int s0 = 0; s0 < a.n_slices; s0 += kAhead) {
+#pragma unroll
+      for (int j = 0; j < kAhead / 2; ++j) {
+        const int s = 2 * j + tid / kBins;
+        if (s0 > 0) ahead[j] = min(slices + s0 + s, last)->bin[tid & (kBins - 1)];
+        all[s][tid & (kBins - 1)] = ahead[j];
+      }
+      __syncthreads();
+      if (tid < kBins) {
+#pragma unroll 8
+        for (int s = 0; s < min(kAhead, a.n_slices - s0); ++s) {
+          const int off = lds.info[s0 + s] & 511;
+          const u64 h = all[s][max(tid - off, 0)];
+          w += off <= tid ? h & ((1ull << kCountShift) - 1) : 0;
+          c += off <= tid ? h >> kCountShift : 0;
+        }
+      }
+      __syncthreads();
+    }
+    if (tid < kBins) {
+      lds.w[tid] = w;
+      lds.bins_c[tid] = c;
+    }
   }
-  __syncthreads();
-  double f = 0.0;
-  u64 w = 0, c = 0;
-  if (tid < kBins) {
-    w = lds.w[tid];
-    c = lds.bins_c[tid];
-    // over the first bin's middle: equal logits there are summed and divided exactly
-    f = exp(-0.125 * tid) * (1.0 / (double)(1ull << kUnitBits));
-    lds.factor[tid] = f;
-  }
-  const double cum_w = scan_bins((double)w * f, lds.dpart);
+  // (over the first bin's middle: equal logits there are summed and divided exactly)
+  const double cum_w = scan_bins((double)w * factor, lds.dpart);
   const u64 cum_c = scan_bins(c, lds.part);
   if (tid < kBins) {
+    lds.factor[tid] = factor;
+    lds.per[tid] = per;
     lds.cum_w[tid] = cum_w;
     lds.cum_c[tid] = cum_c;
+  }
+  if constexpr (!SOLO) {
+    // listed tokens by bin (each slice has as many of the places)
+    if (tid < kBins) lds.sub_c[tid] = 0;
+    __syncthreads();
+    const auto add = [&](int e, float2 y) {
+      const int s = min(e >> a.list_log2, a.n_slices - 1), i = e & ((1 << a.list_log2) - 1);
+      uint32_t f;
+      const bool ok = e >> a.list_log2 < a.n_slices && i < (int)(lds.info[s] >> 18);
+      const int b = ok ? R.bin_of(y.x, f) : kBins;
+      if (b >= lds.covered) return;
+      const int p = (int)(b > 0 ? lds.cum_c[b - 1] : 0) + (int)atomicAdd(&lds.sub_c[b], 1ull);
+      if (p < kCands) lds.cand[p] = (u64)falling(y.x) << 32 | (uint32_t)__float_as_int(y.y);
+    };
+#pragma unroll 1
+    for (int e0 = tid; e0 - tid < a.n_slices << a.list_log2; e0 += kListed * kRowThreads) {
+#pragma unroll
+      for (int j = 0; j < kListed; ++j) add(e0 + j * kRowThreads, listed[j]);
+#pragma unroll
+      for (int j = 0; j < kListed; ++j) {
+        const int e = e0 + (kListed + j) * kRowThreads;
+        listed[j] = min(slices + (e >> a.list_log2), last)->list[e & ((1 << a.list_log2) - 1)];
+      }
+    }
   }
   __syncthreads();
 
@@ -566,86 +875,64 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_k(SampleArgs a) {
   double total = lds.cum_w[kBins - 1];
   const auto below_w = [&](int r) { return r > 0 ? lds.cum_w[r - 1] : 0.0; };
   const auto below_c = [&](int r) { return r > 0 ? (int64_t)lds.cum_c[r - 1] : 0; };
-  // the first bin with fn
-  const auto first = [&](auto fn) {
-    if (tid == 0) lds.pick = kBins - 1;
-    __syncthreads();
-    if (tid < kBins && fn(tid)) atomicMin(&lds.pick, tid);
-    __syncthreads();
-    const int r = lds.pick;
-    __syncthreads();
-    return r;
-  };
   const auto cut = [&](int r, int64_t rank, double units) {
     bin = r;
     n = rank;
     total = below_w(r) + units * lds.factor[r];
   };
-  const auto cut_at = [&](int r, int64_t rank) {
-    if (rank == (int64_t)lds.bins_c[r]) {
-      cut(r, rank, (double)lds.w[r]);
-    } else if (rank > 0) {
-      const auto p = R.pick(r, true, false, (double)rank, rank, false);
-      cut(r, p.rank, p.units);
-    } else {
-      cut(r, 0, 0.0);
-    }
-  };
 
-  const int64_t k = a.k ? a.k[row] : 0;
-  if (k > 0 && k < (int64_t)lds.cum_c[kBins - 1]) {
-    const int r = first([&](int i) { return (int64_t)lds.cum_c[i] >= k; });
-    cut_at(r, k - below_c(r));
-  }
-  const float min_p = a.min_p ? a.min_p[row] : 0.f;
-  if (min_p > 0.f && !__builtin_isinf(m)) {
-    // the bin where weights fall below min_p, and how many of it do not
-    const double low = (double)fminf(min_p, 1.f);
-    const double d = R.bm - __builtin_floor(((double)m * R.inv_T + log(low)) * 8.0);
-    const int r = d < (double)kBins ? max(0, (int)d) : kBins;
-    if (r <= bin) {
-      if (tid == 0) lds.n = 0;
-      __syncthreads();
-      R.each(r, [&](float v, int) {
-        if (exp(((double)v - (double)m) * R.inv_T) >= low) atomicAdd(&lds.n, 1);
-      });
-      __syncthreads();
-      const int64_t keep = lds.n;
-      __syncthreads();
-      if (r < bin || keep < n) cut_at(r, keep);
+  // top-k, min-p, top-p, the draw
+#pragma unroll 1
+  for (int step = 0; step < 4; ++step) {
+    if (step == 0 && (top_k <= 0 || top_k >= (int64_t)lds.cum_c[kBins - 1])) continue;
+    if (step == 1 && (!(min_p > 0.f) || __builtin_isinf(m))) continue;
+    if (step == 2 && !(top_p < 1.f)) continue;
+    Ask q{step <= 1, step <= 2, 0.0, 0};
+    int r = 0;
+    double edge = 0.0;
+    if (step == 1) {
+      // the bin where weights fall below min_p
+      edge = log((double)fminf(min_p, 1.f));
+      const double d = bm - __builtin_floor(((double)m * inv_T + edge) * 8.0);
+      r = d < (double)kBins ? max(0, (int)d) : kBins;
+      if (r > bin) continue;
+      q.most = r == bin ? n : (int64_t)lds.bins_c[r];
+      if (q.most == 0) {   // (all before it weigh enough)
+        if (r < bin) cut(r, 0, 0.0);
+        continue;
+      }
+    } else {
+      const double target = (double)fminf(fmaxf(step == 2 ? top_p : u, 0.f), 1.f) * total;   // (NaN: 0)
+      const bool here = tid >= kBins ? false
+                        : step == 0  ? (int64_t)lds.cum_c[tid] >= top_k
+                        : step == 2 ? c > 0 && lds.cum_w[tid] >= target
+                                    : lds.cum_w[tid] > target;
+      r = min(first_of(here, kBins - 1, lds), bin);
+      q.most = r == bin ? n : (int64_t)lds.bins_c[r];
+      while (q.most == 0 && r > 0) q.most = (int64_t)lds.bins_c[--r];   // (a cut at the head of a bin)
+      q.target = step == 0 ? (double)(top_k - below_c(r)) : (target - below_w(r)) * lds.per[r];
     }
-  }
-  const float top_p = a.p ? a.p[row] : 1.f;
-  if (top_p < 1.f) {
-    const double target = (double)fmaxf(top_p, 0.f) * total;
-    const int r = min(bin, first([&](int i) { return lds.bins_c[i] > 0 && lds.cum_w[i] >= target; }));
-    const int64_t most = r == bin ? n : (int64_t)lds.bins_c[r];
-    if (most > 0) {
-      const auto p = R.pick(r, false, true, (target - below_w(r)) / lds.factor[r], most, false);
+    const auto p = R.pick(r, q, step == 1, edge);
+    if (p.rank < 0) {   // (all of the bin weigh enough)
+      if (r < bin) cut(r, q.most, (double)lds.w[r]);
+      continue;
+    }
+    if (step < 3) {
       cut(r, p.rank, p.units);
-    }
-  }
-  const float u = fminf(fmaxf(a.u[row], 0.f), 1.f);   // (NaN: 0)
-  const double target = (double)u * total;
-  int r = min(bin, first([&](int i) { return lds.cum_w[i] > target; }));
-  int64_t most = r == bin ? n : (int64_t)lds.bins_c[r];
-  while (most == 0 && r > 0) most = (int64_t)lds.bins_c[--r];   // (a cut at the head of a bin)
-  const auto p = R.pick(r, false, false, (target - below_w(r)) / lds.factor[r], most, true);
-  if (tid == 0) {
-    a.next[row] = p.index;
-    if (a.logprob) {
-      // (the first bin's middle over the largest logit)
-      const double top = (0.5 - place_of(m, m, R.rate, R.bm).f) * 0.125;
-      const double z = p.x == m ? 0.0 : ((double)p.x - (double)m) * R.inv_T;
-      a.logprob[row] = (float)(z - top - log(total));
+    } else if (tid == 0) {
+      a.next[row] = min(max(p.index, 0), a.V - 1);
+      if (a.logprob) {
+        // (the first bin's middle over the largest logit)
+        const double top = (0.5 - spot_of(m, rate).f * 0x1p-32) * 0.125;
+        const double z = p.x == m ? 0.0 : ((double)p.x - (double)m) * inv_T;
+        a.logprob[row] = (float)(z - top - log(total));
+      }
     }
   }
 }
 
 static int slice_elements(int64_t rows, int64_t V) {
-  (void)rows;
-  (void)V;
-  return 32;
+  return rows * V >= ((int64_t)1 << 22) || V > kMaxSlices * 2048 ? 32 : 8;
 }
 static int64_t slices_of(int64_t rows, int64_t V) {
   const int64_t slice = 256 * slice_elements(rows, V);
@@ -673,7 +960,7 @@ pipo_status pipo_op_sample(const float* logits, int64_t ld, const float* tempera
               (long long)rows, (long long)V, (long long)ld);
     return PIPO_ERR_ARG;
   }
-  if (V > kMaxV || rows >= ((int64_t)1 << 22)) {
+  if (V > kMaxV || rows >= ((int64_t)1 << 21)) {
     set_error("sample: %lld rows of %lld logits", (long long)rows, (long long)V);
     return PIPO_ERR_UNSUPPORTED;
   }
@@ -691,15 +978,18 @@ pipo_status pipo_op_sample(const float* logits, int64_t ld, const float* tempera
   a.slices = static_cast<Slice*>(workspace);
   a.V = (int)V;
   a.n_slices = (int)slices_of(rows, V);
-  a.slice = 256 * slice_elements(rows, V);
-  a.vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && ld % 4 == 0;
+  a.list_log2 = 31 - __builtin_clz((unsigned)std::min(kListMax, kCands / a.n_slices));
   const int64_t need = pipo_op_sample_workspace_bytes(rows, V);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 || need == 0 ||
       workspace_bytes < need) {
     launch(sample_rows_k<true>, dim3((unsigned)rows), dim3(kRowThreads), 0, st, a);
   } else {
-    launch(sample_slices_k<32>, dim3((unsigned)(rows * a.n_slices)), dim3(256), 0, st, a);
+    const dim3 g((unsigned)(rows * a.n_slices));
+    if (slice_elements(rows, V) == 32)
+      launch(sample_slices_k<32>, g, dim3(256), 0, st, a);
+    else
+      launch(sample_slices_k<8>, g, dim3(256), 0, st, a);
     launch(sample_rows_k<false>, dim3((unsigned)rows), dim3(kRowThreads), 0, st, a);
   }
   PIPO_HIP_TRY(hipGetLastError());

@@ -24,12 +24,17 @@ struct Attn8 {
   int64_t ldq, ldo, M;
   int H, G, max_q, max_len, window, max_prefix;
   float cap;
-  int chunk;        // keys of a split
-  int splits;       // of a row's partials in `part`
+  int few_cols;               // up to this many are attn8_few_k's, or none
+  int chunk_few, chunk_many;  // keys of a split, by the sequence's columns
+  int splits;                 // of a row's partials in `part`
   bool q_vec, o_vec;
 };
 
-constexpr int kBlock = 32;      // keys that a wave takes at a time
+// Up to this many columns a sequence is attn8_few_k's, above it attn8_many_k's; all of them
+// where every row of the call may be one of max_q equal shares, which saves a launch.
+constexpr int kFewCols = 64;
+constexpr int kBlock = 32;      // keys that a wave of few columns takes at a time
+constexpr int kManyCols = 128, kManyKeys = 64;
 constexpr int kMaxSplits = 64;  // a wave's lanes, where they are joined
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^14: as a half it keeps 11 bits down to 2^-28
@@ -62,21 +67,24 @@ __device__ __forceinline__ Seen seen_by(const Attn8& a, const Seq8& s, int j) {
   w.lo = a.window > 0 ? (int)min(max(after - a.window, (int64_t)0), (int64_t)s.len) : 0;
   return w;
 }
-// blocks that rows j0 .. j1 see: [0, head) and [from, from + n - head), n in all
+// blocks of KEYS keys that rows j0 .. j1 see: [0, head) and [from, from + n - head), n in all
 struct Blocks {
   int head, from, n;
+  __device__ __forceinline__ int operator()(int b) const { return b < head ? b : b - head + from; }
 };
+template <int KEYS>
 __device__ __forceinline__ Blocks blocks_of(const Attn8& a, const Seq8& s, int j0, int j1) {
   Blocks b;
-  const int pre = (s.pre + kBlock - 1) / kBlock;
-  b.from = seen_by(a, s, j0).lo / kBlock;
+  const int pre = (s.pre + KEYS - 1) / KEYS;
+  b.from = seen_by(a, s, j0).lo / KEYS;
   b.head = min(pre, b.from);
-  b.n = b.head + max(max(pre, (seen_by(a, s, j1).hi + kBlock - 1) / kBlock) - b.from, 0);
+  b.n = b.head + max(max(pre, (seen_by(a, s, j1).hi + KEYS - 1) / KEYS) - b.from, 0);
   return b;
 }
-__device__ __forceinline__ int splits_of(const Attn8& a, const Seq8& s) {
-  const int n = s.rows > 0 ? blocks_of(a, s, 0, s.rows - 1).n : 0;
-  return min(max(1, (int)(((int64_t)n * kBlock + a.chunk - 1) / a.chunk)), a.splits);
+template <int KEYS>
+__device__ __forceinline__ int splits_of(const Attn8& a, const Seq8& s, int chunk) {
+  const int n = s.rows > 0 ? blocks_of<KEYS>(a, s, 0, s.rows - 1).n : 0;
+  return min(max(1, (int)(((int64_t)n * KEYS + chunk - 1) / chunk)), a.splits);
 }
 
 template <int D>
@@ -179,8 +187,8 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq8 s = sequence(a, si);
   const int cols = s.rows * a.G;
-  if (16 * ct >= cols) return;
-  const int ns = splits_of(a, s);
+  if (16 * ct >= cols || cols > a.few_cols) return;
+  const int ns = splits_of<kBlock>(a, s, a.chunk_few);
   if (sp >= ns) return;
   const int r = lane & 15, g = lane >> 4;
 
@@ -192,10 +200,10 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int at = s.len - s.nq + qj;   // its position
   const int j0 = 16 * ct / a.G, j1 = min(s.rows - 1, (16 * ct + 15) / a.G);
   const int all_lo = seen_by(a, s, j1).lo, all_hi = seen_by(a, s, j0).hi;
-  const Blocks blocks = blocks_of(a, s, j0, j1);
-  const int per = a.chunk / kBlock, b1 = (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per);
+  const Blocks blocks = blocks_of<kBlock>(a, s, j0, j1);
+  const int per = a.chunk_few / kBlock, b1 = (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per);
   int b = sp * per + wave;
-  const auto key_of = [&](int b) { return kBlock * (b < blocks.head ? b : b - blocks.head + blocks.from); };
+  const auto key_of = [&](int b) { return kBlock * blocks(b); };
 
   // lane 2 i + j holds the page and the scales of tile j of the wave's i-th block, 32
   // blocks at a time
@@ -355,6 +363,374 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   }
 }
 
+// Many columns: a workgroup is one or two teams of four waves of 32 columns each
+// on (sequence, key/value head, 128 columns, split).  Two teams take the split's
+// keys by turns, 64 at a time, and meet in LDS at the end.  In a team each wave
+// unpacks a tile of the next block into LDS, in operand order and with its scales, while
+// all of them work on this one, so a block is unpacked once for 128 columns and every LDS
+// access is a wave's contiguous kilobyte.  Weights are rounded to a half, and it is the
+// rounded ones that are added up to divide by.
+
+// The t-th column tile of the launch: its sequence (-1: none) and which of the
+// sequence's tiles.  Only sequences of many columns have tiles.  Up to 64 sequences go by
+// their keys, the most first, and of a sequence the tiles with the most keys.
+struct Place8 {
+  int seq, tile;
+};
+__device__ __forceinline__ int many_tiles(const Attn8& a, int i) {
+  const int cols = sequence(a, i).rows * a.G;
+  return cols > a.few_cols ? (cols + kManyCols - 1) / kManyCols : 0;
+}
+__device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
+  const int n = a.c.n_seq, lane = threadIdx.x & 63;
+  if (n <= 64) {
+    const int tiles = lane < n ? many_tiles(a, lane) : 0, keys = tiles ? a.kv_len[lane] : 0;
+    int before = 0;
+    for (int i = 0; i < n; ++i) {
+      const int k = __builtin_amdgcn_readlane(keys, i), w = __builtin_amdgcn_readlane(tiles, i);
+      before += k > keys || (k == keys && i < lane) ? w : 0;
+    }
+    const uint64_t hit = __ballot(t >= before && t < before + tiles);
+    if (!hit) return Place8{-1, 0};
+    const int i = __ffsll((unsigned long long)hit) - 1;
+    return Place8{i, __builtin_amdgcn_readlane(before + tiles - 1, i) - t};
+  }
+  const int each = (n + 63) / 64, first = lane * each, last = min(n, first + each);
+  int sum = 0;
+  for (int i = first; i < last; ++i) sum += many_tiles(a, i);
+  int end = sum;  // of this lane's tiles
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(end, d, 64);
+    if (lane >= d) end += y;
+  }
+  const uint64_t hit = __ballot(t >= end - sum && t < end);
+  if (!hit) return Place8{-1, 0};
+  const int src = __ffsll((unsigned long long)hit) - 1;
+  int r = t - __builtin_amdgcn_readlane(end - sum, src);
+  for (int i = src * each;; ++i) {  // (ends: r is below the sum of these)
+    const int tiles = many_tiles(a, i);
+    if (r < tiles) return Place8{i, tiles - 1 - r};
+    r -= tiles;
+  }
+}
+
+// K operands [tile][kk][lane], V operands [pair of tiles][fragment][lane], and which tiles
+// are pages'
+template <int D>
+struct ManyStage8 {
+  h8 k[kManyKeys / 16][D / 32][64];
+  h8 v[kManyKeys / 32][D / 16][64];
+  uint32_t valid[kManyKeys / 16];
+};
+template <int D, int TEAMS>
+struct Many8Lds {
+  static constexpr int ROW = D + 4;  // floats of a column's sums, where the teams meet
+  union {
+    ManyStage8<D> st[TEAMS][2];
+    float sums[TEAMS - 1 ? kManyCols : 1][ROW];
+  };
+  float2 rl[TEAMS - 1 ? kManyCols : 1];
+};
+
+template <int D, bool INT8, bool MOD, int TEAMS>
+__global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void attn8_many_k(
+    Attn8 a) {
+  constexpr int KK = D / 32, NF = D / 16, C = D / 64, T = kManyKeys / 16, U = 2;
+  using Stage = ManyStage8<D>;
+  __shared__ Many8Lds<D, TEAMS> lds;
+  const int kh = blockIdx.x % a.c.Hkv, sp = blockIdx.y;
+  const Place8 place = place_of(a, blockIdx.x / a.c.Hkv);
+  if (place.seq < 0) return;
+  const int si = __builtin_amdgcn_readfirstlane(place.seq);
+  const int ct = __builtin_amdgcn_readfirstlane(place.tile);
+  const Seq8 s = sequence(a, si);
+  const int cols = s.rows * a.G;
+  const int ns = splits_of<kManyKeys>(a, s, a.chunk_many);
+  if (sp >= ns) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
+  const int team = __builtin_amdgcn_readfirstlane(tid >> 8);
+  const int r = lane & 15, g = lane >> 4;
+  Stage* const st = lds.st[team];
+
+  const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
+  const int j0 = kManyCols * ct / a.G, j1 = min(s.rows - 1, (kManyCols * ct + kManyCols - 1) / a.G);
+  const Blocks blocks = blocks_of<kManyKeys>(a, s, j0, j1);
+  const int per = a.chunk_many / kManyKeys, b0 = sp * per;
+  const int n_blocks = max(0, (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per) - b0);
+  // this team's are blocks team, team + TEAMS .., and all waves go through as many
+  const int turns = (n_blocks + TEAMS - 1) / TEAMS, mine = (n_blocks + TEAMS - 1 - team) / TEAMS;
+  const auto key_of = [&](int blk) { return kManyKeys * blocks(b0 + TEAMS * blk + team); };
+  // keys that all of the wave's columns see, and that any does
+  const int w0 = c0 / a.G, w1 = min(s.rows - 1, (c0 + 31) / a.G);
+  const bool idle = c0 >= cols;
+  const int all_lo = idle ? 0 : seen_by(a, s, w1).lo, all_hi = idle ? 0 : seen_by(a, s, w0).hi;
+  const int any_lo = idle ? 0 : seen_by(a, s, w0).lo, any_hi = idle ? 0 : seen_by(a, s, w1).hi;
+
+  // this wave's tile of the next block, on its way
+  u32x4 kw[C], vw[C];
+  float ks, vs;
+  uint32_t ok;
+  int exist;   // keys of the tile that do
+  // lane i holds the page and the scales of its tile in the team's block i, 64 at a time
+  const int32_t* table = a.c.table + si * a.c.stride;
+  int pages = -1;
+  float2 scales = make_float2(1.f, 1.f);
+  const auto fetch = [&](int blk) {
+    if ((blk & 63) == 0) {
+      pages = -1;
+      scales = make_float2(1.f, 1.f);
+      if (blk + lane < mine) {
+        const int pos = key_of(blk + lane) + 16 * wave;
+        if (pos < s.len) pages = table[pos >> a.c.ps_log2];
+        if (pages < 0 || pages >= a.c.n_pages) pages = -1;
+        if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
+      }
+    }
+    const int pos = key_of(blk) + 16 * wave;
+    const int page = __builtin_amdgcn_readlane(pages, blk & 63);
+    ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.x), blk & 63));
+    vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.y), blk & 63));
+    ok = page >= 0;
+    exist = ok ? s.len - pos : 0;
+    const uint8_t* tile = tile8_at<D>(a.c, ok ? page : 0, kh, pos) + 16 * lane;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      kw[c] = *reinterpret_cast<const u32x4*>(tile + 1024 * c);
+      vw[c] = *reinterpret_cast<const u32x4*>(tile + 16 * D + 1024 * c);
+    }
+  };
+  const auto unpack = [&](Stage& x) {
+    if (exist < 16) {   // codes of keys that do not exist may be anything
+      const int n = min(max(exist - 4 * g, 0), 4);
+      const uint32_t keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
+#pragma unroll
+      for (int c = 0; c < C; ++c) vw[c] &= keep;
+    }
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      x.k[wave][kk][lane] = halves8<INT8, false>(kw[kk / 2][2 * (kk % 2)], kw[kk / 2][2 * (kk % 2) + 1], ks, ks);
+#pragma unroll
+    for (int n = 0; n < NF; n += 2) {
+      const h8 y = halves8<INT8, false>(vw[n / 4][n % 4], vw[n / 4][n % 4 + 1], vs, vs);
+      reinterpret_cast<h4*>(&x.v[wave / 2][n][lane])[wave % 2] = h4{y[0], y[1], y[2], y[3]};
+      reinterpret_cast<h4*>(&x.v[wave / 2][n + 1][lane])[wave % 2] = h4{y[4], y[5], y[6], y[7]};
+    }
+    if (lane == 0) x.valid[wave] = ok;
+  };
+
+  h8 qf[U][KK];
+  float slope[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int col = c0 + 16 * u + r, qj = col / a.G, h = kh * a.G + col % a.G;
+    slope[u] = MOD && a.slopes && col < cols ? a.slopes[h] * kLog2e : 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qf[u][kk] = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
+  }
+  const Scores f = scores_of(a);
+  f4 acc[U][NF], sum[U];
+  float R[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    R[u] = -INFINITY;
+    sum[u] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NF; ++n) acc[u][n] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+  const h8 ones = h8(1);
+
+  const auto compute = [&](const Stage& x, int k0, auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+    f4 y[U][T];   // scores; MOD: in units of log 2
+    h8 kf[2][KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kf[0][kk] = x.k[0][kk][lane];
+#pragma unroll
+    for (int j = 0; j < T; ++j) {
+      if (j + 1 < T) {
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[(j + 1) & 1][kk] = x.k[j + 1][kk][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (these loads travel beside this tile's work)
+#pragma unroll
+      for (int u = 0; u < U; ++u) y[u][j] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int u = 0; u < U; ++u) y[u][j] = mfma16(kf[j & 1][kk], qf[u][kk], y[u][j]);
+    }
+    if constexpr (MOD || EDGE) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int col = c0 + 16 * u + r, qj = col / a.G, at = s.len - s.nq + qj;
+      Seen see = Seen{0, 0};
+      if (col < cols) see = seen_by(a, s, qj);
+      const int pre = col < cols ? s.pre : 0;
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = k0 + 16 * j + 4 * g + e;
+          float v = y[u][j][e];
+          if constexpr (MOD) {
+            const int far = at - key;
+            v = score(f, v, slope[u], (float)(far < 0 ? -far : far));
+          }
+          if constexpr (EDGE) {
+            const bool in = x.valid[j] && ((key >= see.lo && key < see.hi) || key < pre);
+            v = in ? v : -INFINITY;
+          }
+          y[u][j][e] = v;
+        }
+    }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr float unit = MOD ? 1.f : kLog2e;
+    float shift[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < T; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, y[u][j][e]);
+      const float Rn = fmaxf(R[u], cols_max(top) * unit);
+      const float Rs = EDGE && Rn == -INFINITY ? 0.f : Rn;
+      const float alpha = __builtin_amdgcn_exp2f(R[u] - Rs);
+      R[u] = Rn;
+      shift[u] = kPBits - Rs;
+      if (__any(alpha != 1.f)) {
+        sum[u] *= alpha;
+#pragma unroll
+        for (int n = 0; n < NF; ++n) acc[u][n] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < T / 2; ++t) {
+      h8 vf[NF / 2], pf[U];
+#pragma unroll
+      for (int n = 0; n < NF / 2; ++n) vf[n] = x.v[t][n][lane];
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            pf[u][4 * jj + e] =
+                (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(y[u][2 * t + jj][e], unit, shift[u]));
+        sum[u] = mfma16(ones, pf[u], sum[u]);
+      }
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) acc[u][n] = mfma16(vf[n % (NF / 2)], pf[u], acc[u][n]);
+        if (n < NF / 2) vf[n] = x.v[t][n + NF / 2][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (mine > 0) {
+    fetch(0);
+    unpack(st[0]);
+  }
+  __syncthreads();
+  // blocks that every column of the wave sees whole, and others, in turn
+  int blk = 0;
+  const auto run = [&](auto edge_c) {
+    constexpr bool EDGE = decltype(edge_c)::value;
+#pragma unroll 1
+    for (; blk < turns; ++blk) {
+      const Stage& x = st[blk & 1];
+      const int k0 = key_of(blk), k1 = k0 + kManyKeys;
+      bool whole = false;
+      if (blk < mine) {
+        uint32_t v = 1;
+#pragma unroll
+        for (int j = 0; j < T; ++j) v &= x.valid[j];
+        whole = __builtin_amdgcn_readfirstlane(v) && ((k0 >= all_lo && k1 <= all_hi) || k1 <= s.pre);
+      }
+      if (whole == EDGE) return;
+      if (blk + 1 < mine) fetch(blk + 1);
+      if (!EDGE || (blk < mine && ((k1 > any_lo && k0 < any_hi) || (k0 < s.pre && !idle))))
+        compute(x, k0, edge_c);
+      if (blk + 1 < mine) unpack(st[(blk + 1) & 1]);
+      __syncthreads();
+    }
+  };
+#pragma unroll 1
+  while (blk < turns) {
+    run(std::false_type{});
+    run(std::true_type{});
+  }
+
+  // element e of acc[u][n]: dimension 16 n + 4 g + e of column c0 + 16 u + r.  The
+  // second team's sums go to LDS (every block there is read), the first adds them.
+  float l[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    l[u] = sum[u][0];
+    const int c = 32 * wave + 16 * u + r;
+    if (TEAMS == 2 && team == 1) {
+#pragma unroll
+      for (int n = 0; n < NF; ++n) *reinterpret_cast<f4*>(&lds.sums[c][16 * n + 4 * g]) = acc[u][n];
+      if (g == 0) lds.rl[c] = make_float2(R[u], l[u]);
+    }
+  }
+  if constexpr (TEAMS == 2) {
+    __syncthreads();
+    if (team == 1) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = 32 * wave + 16 * u + r;
+      const float2 rl = lds.rl[c];
+      const float Rn = fmaxf(R[u], rl.x), Rs = Rn == -INFINITY ? 0.f : Rn;
+      const float f0 = __builtin_amdgcn_exp2f(R[u] - Rs), f1 = __builtin_amdgcn_exp2f(rl.x - Rs);
+      R[u] = Rn;
+      l[u] = l[u] * f0 + rl.y * f1;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        const f4 y = *reinterpret_cast<const f4*>(&lds.sums[c][16 * n + 4 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[u][n][e] = acc[u][n][e] * f0 + y[e] * f1;
+      }
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int col = c0 + 16 * u + r;
+    const float L = l[u];
+    if (col >= cols) continue;
+    const int m = s.row0 + col / a.G, h = kh * a.G + col % a.G;
+    if (ns == 1) {
+      const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+      uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) {
+        uint16_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = f2h(acc[u][n][e] * inv);
+        if (a.o_vec) {
+          *reinterpret_cast<u32x2*>(o + 16 * n + 4 * g) =
+              u32x2{(uint32_t)v[0] | ((uint32_t)v[1] << 16), (uint32_t)v[2] | ((uint32_t)v[3] << 16)};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[16 * n + 4 * g + e] = v[e];
+        }
+      }
+    } else {
+      const int64_t p = ((int64_t)m * a.H + h) * a.splits + sp;
+#pragma unroll
+      for (int n = 0; n < NF; ++n) *reinterpret_cast<f4*>(a.part + p * D + 16 * n + 4 * g) = acc[u][n];
+      if (g == 0) a.part_rl[p] = make_float2(R[u], L);
+    }
+  }
+}
+
 // sequence that holds row m (-1: none): the last i with q_start[i] <= m, 64
 // candidates at a time
 __device__ __forceinline__ int seq_of_row(const Attn8& a, int m) {
@@ -379,7 +755,8 @@ __global__ __launch_bounds__(256) void attn8_merge_k(Attn8 a) {
   const int i = seq_of_row(a, m);
   if (i < 0 || h >= a.H) return;
   const Seq8 s = sequence(a, i);
-  const int ns = splits_of(a, s);
+  const int ns = s.rows * a.G <= a.few_cols ? splits_of<kBlock>(a, s, a.chunk_few)
+                                            : splits_of<kManyKeys>(a, s, a.chunk_many);
   if (ns == 1 || m - s.row0 >= s.rows) return;
   const int64_t at = ((int64_t)m * a.H + h) * a.splits;
   const float2 rl = lane < ns ? a.part_rl[at + lane] : make_float2(-INFINITY, 0.f);
@@ -401,28 +778,55 @@ __global__ __launch_bounds__(256) void attn8_merge_k(Attn8 a) {
   for (int n = 0; n < N; ++n) o[64 * n + lane] = f2h(L > 0.f ? A[n] / L : (L == L ? 0.f : L));
 }
 
+static int64_t col_tiles(int64_t max_q, int G, int tile) { return (max_q * G + tile - 1) / tile; }
+
 // keys that a sequence's rows see at most, in whole blocks
-static int64_t seen_keys(const pipo_attn_scores* f, int64_t max_q, int64_t max_len) {
-  const auto up = [](int64_t n) { return (n + kBlock - 1) / kBlock * kBlock; };
+static int64_t seen_keys(const pipo_attn_scores* f, int64_t max_q, int64_t max_len, int block) {
+  const auto up = [&](int64_t n) { return (n + block - 1) / block * block; };
   if (!f || f->window <= 0) return up(max_len);
-  return std::min(up(max_len), up(f->prefix ? f->max_prefix : 0) + up(f->window + max_q) + kBlock);
+  return std::min(up(max_len), up(f->prefix ? f->max_prefix : 0) + up(f->window + max_q) + block);
 }
 
-constexpr int kCUs = 256, kMinKeys = 256, kSplitKeys = 768;
-struct Plan8 {
-  int waves, chunk, splits;
-};
-static Plan8 plan_attn8(const pipo_kv8_pages* c, const pipo_attn_scores* f, int n_heads, int64_t max_q,
-                        int64_t max_len) {
-  const int G = n_heads / c->n_kv_heads;
-  const int64_t keys = seen_keys(f, max_q, max_len);
-  const int64_t wgs = (int64_t)c->n_seq * c->n_kv_heads * ((max_q * G + 15) / 16);
-  Plan8 p;
-  p.waves = wgs <= kCUs ? 8 : 4;
-  int64_t S = keys < kSplitKeys ? 1 : std::min(kCUs / wgs, keys / kMinKeys);
+// keys of each of S parts, in whole blocks
+static int chunk_of(int64_t keys, int64_t S, int block) {
   S = std::max<int64_t>(1, std::min<int64_t>(S, kMaxSplits));
-  p.chunk = (int)std::max<int64_t>(kBlock, ((keys + S - 1) / S + kBlock - 1) / kBlock * kBlock);
-  p.splits = (int)std::max<int64_t>(1, (keys + p.chunk - 1) / p.chunk);
+  return (int)std::max<int64_t>(block, ((keys + S - 1) / S + block - 1) / block * block);
+}
+
+constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
+struct Plan8 {
+  bool few, many;   // sequences that may be of either kind
+  int waves;        // of a workgroup for those of few columns
+  int teams;        // of a workgroup for the others
+  int64_t tiles;    // of 128 columns they have at most
+  int chunk_few, chunk_many, splits_few, splits_many;
+  int splits() const { return std::max(few ? splits_few : 1, many ? splits_many : 1); }
+};
+static Plan8 plan_attn8(const pipo_kv8_pages* c, const pipo_attn_scores* f, int n_heads, int64_t M,
+                        int64_t max_q, int64_t max_len) {
+  const int G = n_heads / c->n_kv_heads;
+  Plan8 p;
+  p.many = max_q * G > kFewCols;
+  p.few = !p.many || (G <= kFewCols && M < c->n_seq * max_q);
+  const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, kFewCols / G));
+  // (with many columns about, most of the others have one row)
+  const int64_t q = p.many ? 1 : few_q, wgs = (int64_t)c->n_seq * c->n_kv_heads * col_tiles(q, G, 16);
+  const int64_t few = seen_keys(f, few_q, max_len, kBlock), many = seen_keys(f, max_q, max_len, kManyKeys);
+  p.waves = wgs <= kCUs ? 8 : 4;
+  p.chunk_few = chunk_of(few, few < kSplitFew ? 1 : std::min(kCUs / wgs, few / kMinFew), kBlock);
+  p.tiles = std::min(c->n_seq * col_tiles(max_q, G, kManyCols), M * G / kManyCols + c->n_seq);
+  // (of n columns above 64, at most n / 64.5)
+  static_assert(kManyCols == 2 * kFewCols, "the bound of a sequence's tiles");
+  if (p.few) p.tiles = std::min(p.tiles, 2 * M * G / 129);
+  const int64_t tiles = std::max<int64_t>(1, p.tiles * c->n_kv_heads);
+  p.chunk_many = chunk_of(many, std::min((kCUs + tiles - 1) / tiles, many / kMinMany), kManyKeys);
+  if (M >= (1 << 23)) {   // (a grid of M workgroups)
+    p.chunk_few = chunk_of(few, 1, kBlock);
+    p.chunk_many = chunk_of(many, 1, kManyKeys);
+  }
+  p.teams = tiles > 3 * kCUs ? 1 : 2;
+  p.splits_few = (int)std::max<int64_t>(1, (few + p.chunk_few - 1) / p.chunk_few);
+  p.splits_many = (int)std::max<int64_t>(1, (many + p.chunk_many - 1) / p.chunk_many);
   return p;
 }
 
@@ -457,13 +861,22 @@ static pipo_status check_attn8(const char* what, const pipo_kv8_pages* c, const 
 
 template <int D, bool INT8, bool MOD>
 static void launch_attn8(const Attn8& a, const Plan8& p, hipStream_t st) {
-  const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), (unsigned)p.splits,
-               (unsigned)(((int64_t)a.max_q * a.G + 15) / 16));
-  if (p.waves == 8)
-    launch(attn8_few_k<D, INT8, MOD, 8>, g, dim3(512), 0, st, a);
-  else
-    launch(attn8_few_k<D, INT8, MOD, 4>, g, dim3(256), 0, st, a);
-  if (p.splits > 1)
+  if (p.few) {
+    const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, p.many ? kFewCols : INT32_MAX);
+    const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), (unsigned)p.splits_few, (unsigned)((cols + 15) / 16));
+    if (p.waves == 8)
+      launch(attn8_few_k<D, INT8, MOD, 8>, g, dim3(512), 0, st, a);
+    else
+      launch(attn8_few_k<D, INT8, MOD, 4>, g, dim3(256), 0, st, a);
+  }
+  if (p.many && p.tiles > 0) {
+    const dim3 g((unsigned)(a.c.Hkv * p.tiles), (unsigned)p.splits_many);
+    if (p.teams == 2)
+      launch(attn8_many_k<D, INT8, MOD, 2>, g, dim3(512), 0, st, a);
+    else
+      launch(attn8_many_k<D, INT8, MOD, 1>, g, dim3(256), 0, st, a);
+  }
+  if (p.splits() > 1)
     launch(attn8_merge_k<D>, dim3((unsigned)a.M, (unsigned)((a.H + 3) / 4)), dim3(256), 0, st, a);
 }
 
@@ -481,7 +894,7 @@ int64_t pipo_op_attn_kv8_pages_workspace_bytes(const pipo_kv8_pages* c, const pi
       check_attn8("attn_kv8_pages", c, f, n_heads, M, max_q, max_len) != PIPO_OK)
     return 0;
   return partial_bytes8(M, n_heads, c->head_dim,
-                        plan_attn8(c, f, n_heads, std::min<int64_t>(max_q, M), max_len).splits);
+                        plan_attn8(c, f, n_heads, M, std::min<int64_t>(max_q, M), max_len).splits());
 }
 
 pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* c, int32_t layer, const pipo_attn_scores* f,
@@ -517,14 +930,16 @@ pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* c, int32_t layer, const
   a.G = n_heads / c->n_kv_heads;
   a.max_q = (int)std::min<int64_t>(max_q, M);
   a.max_len = max_len;
-  Plan8 p = plan_attn8(c, f, n_heads, a.max_q, max_len);
+  Plan8 p = plan_attn8(c, f, n_heads, M, a.max_q, max_len);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0 ||
-      workspace_bytes < partial_bytes8(M, n_heads, c->head_dim, p.splits)) {
-    p.chunk = std::max(kBlock, (max_len + kBlock - 1) / kBlock * kBlock);
-    p.splits = 1;
+      workspace_bytes < partial_bytes8(M, n_heads, c->head_dim, p.splits())) {
+    p.chunk_few = p.chunk_many = std::max(kManyKeys, (max_len + kManyKeys - 1) / kManyKeys * kManyKeys);
+    p.splits_few = p.splits_many = 1;
   }
-  a.chunk = p.chunk;
-  a.splits = p.splits;
+  a.few_cols = p.few ? kFewCols : 0;
+  a.chunk_few = p.chunk_few;
+  a.chunk_many = p.chunk_many;
+  a.splits = p.splits();
   a.part_rl = reinterpret_cast<float2*>(a.part + M * n_heads * a.splits * c->head_dim);
   a.q_vec = reinterpret_cast<uintptr_t>(q) % 16 == 0 && ldq % 8 == 0;
   a.o_vec = reinterpret_cast<uintptr_t>(o) % 8 == 0 && ldo % 4 == 0;

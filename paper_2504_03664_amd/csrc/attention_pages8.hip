@@ -141,12 +141,12 @@ __device__ __forceinline__ Scores scores_of(const Attn8& a) {
 }
 // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by a few 2^-24 of the cap, in a
 // number whose exponential is taken
-__device__ __forceinline__ float score(const Scores& f, float x, float slope, float far) {
+__device__ __forceinline__ float score(const Scores& f, float x) {
   float y = x * kLog2e;
   if (f.cap_in > 0.f)
     y = __builtin_fmaf(-2.f * f.cap_out,
                        __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * f.cap_in) + 1.f), f.cap_out);
-  return __builtin_fmaf(-slope, far, y);
+  return y;
 }
 
 // result of a column: straight to o, or a partial
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
       for (int e = 0; e < 4; ++e) {
         if constexpr (MOD) {
           const int far = at - (key0 + 16 * j + 4 * g + e);
-          y[j][e] = score(f, d[e] * x.ks[j], slope, (float)(far < 0 ? -far : far));
+          y[j][e] = __builtin_fmaf(-slope, (float)(far < 0 ? -far : far), score(f, d[e] * x.ks[j]));
         } else {
           y[j][e] = d[e] * (x.ks[j] * kLog2e);
         }
@@ -416,22 +416,35 @@ __device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
 }
 
 // K operands [tile][kk][lane], V operands [pair of tiles][fragment][lane], and which tiles
-// are pages'
+// are pages', of two blocks by turns: one is read while the next is written
 template <int D>
 struct ManyStage8 {
-  h8 k[kManyKeys / 16][D / 32][64];
-  h8 v[kManyKeys / 32][D / 16][64];
-  uint32_t valid[kManyKeys / 16];
+  h8 k[2][kManyKeys / 16][D / 32][64];
+  h8 v[2][kManyKeys / 32][D / 16][64];
+  uint32_t valid[2][kManyKeys / 16];
 };
 template <int D, int TEAMS>
 struct Many8Lds {
   static constexpr int ROW = D + 4;  // floats of a column's sums, where the teams meet
   union {
-    ManyStage8<D> st[TEAMS][2];
+    ManyStage8<D> st[TEAMS];
     float sums[TEAMS - 1 ? kManyCols : 1][ROW];
   };
   float2 rl[TEAMS - 1 ? kManyCols : 1];
+  uint32_t arrived[TEAMS];  // waves, at the team's barriers so far
 };
+
+// A barrier of a team's four waves, the n-th (from 1): two teams that had the workgroup's
+// would go through the same phases side by side.  Each wave counts itself in behind its LDS
+// accesses and waits for the others, which are on the CU too and come to as many barriers.
+__device__ __forceinline__ void team_barrier(uint32_t* arrived, int n) {
+  __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, true));
+  asm volatile("" ::: "memory");
+  if ((threadIdx.x & 63) == 0) __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  while (__hip_atomic_load(arrived, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) < 4u * n)
+    __builtin_amdgcn_s_sleep(1);
+  asm volatile("" ::: "memory");
+}
 
 template <int D, bool INT8, bool MOD, int TEAMS>
 __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))) void attn8_many_k(
@@ -452,32 +465,31 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6) & 3;
   const int team = __builtin_amdgcn_readfirstlane(tid >> 8);
   const int r = lane & 15, g = lane >> 4;
-  Stage* const st = lds.st[team];
+  Stage& st = lds.st[team];
 
   const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
   const int j0 = kManyCols * ct / a.G, j1 = min(s.rows - 1, (kManyCols * ct + kManyCols - 1) / a.G);
   const Blocks blocks = blocks_of<kManyKeys>(a, s, j0, j1);
   const int per = a.chunk_many / kManyKeys, b0 = sp * per;
   const int n_blocks = max(0, (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per) - b0);
-  // this team's are blocks team, team + TEAMS .., and all waves go through as many
-  const int turns = (n_blocks + TEAMS - 1) / TEAMS, mine = (n_blocks + TEAMS - 1 - team) / TEAMS;
+  // this team's are blocks team, team + TEAMS ..
+  const int mine = (n_blocks + TEAMS - 1 - team) / TEAMS;
   const auto key_of = [&](int blk) { return kManyKeys * blocks(b0 + TEAMS * blk + team); };
-  // keys that all of the wave's columns see, and that any does
+  // keys that all of the wave's columns see
   const int w0 = c0 / a.G, w1 = min(s.rows - 1, (c0 + 31) / a.G);
   const bool idle = c0 >= cols;
   const int all_lo = idle ? 0 : seen_by(a, s, w1).lo, all_hi = idle ? 0 : seen_by(a, s, w0).hi;
-  const int any_lo = idle ? 0 : seen_by(a, s, w0).lo, any_hi = idle ? 0 : seen_by(a, s, w1).hi;
 
-  // this wave's tile of the next block, on its way
+  // this wave's tile of blocks to come, on its way: keys of one, values of the one before
   u32x4 kw[C], vw[C];
-  float ks, vs;
-  uint32_t ok;
-  int exist;   // keys of the tile that do
+  float ks = 1.f, vs = 1.f;
+  bool k_ok = false;
+  int exist = 0;   // of vw's keys
   // lane i holds the page and the scales of its tile in the team's block i, 64 at a time
   const int32_t* table = a.c.table + si * a.c.stride;
   int pages = -1;
   float2 scales = make_float2(1.f, 1.f);
-  const auto fetch = [&](int blk) {
+  const auto fetch_k = [&](int blk) {
     if ((blk & 63) == 0) {
       pages = -1;
       scales = make_float2(1.f, 1.f);
@@ -488,20 +500,28 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
         if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
       }
     }
-    const int pos = key_of(blk) + 16 * wave;
     const int page = __builtin_amdgcn_readlane(pages, blk & 63);
     ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.x), blk & 63));
-    vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.y), blk & 63));
-    ok = page >= 0;
-    exist = ok ? s.len - pos : 0;
-    const uint8_t* tile = tile8_at<D>(a.c, ok ? page : 0, kh, pos) + 16 * lane;
+    k_ok = page >= 0;
+    const uint8_t* tile = tile8_at<D>(a.c, k_ok ? page : 0, kh, key_of(blk) + 16 * wave) + 16 * lane;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      kw[c] = *reinterpret_cast<const u32x4*>(tile + 1024 * c);
-      vw[c] = *reinterpret_cast<const u32x4*>(tile + 16 * D + 1024 * c);
-    }
+    for (int c = 0; c < C; ++c) kw[c] = *reinterpret_cast<const u32x4*>(tile + 1024 * c);
   };
-  const auto unpack = [&](Stage& x) {
+  const auto fetch_v = [&](int blk) {   // (before fetch_k of a block of the next 64)
+    const int pos = key_of(blk) + 16 * wave, page = __builtin_amdgcn_readlane(pages, blk & 63);
+    vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.y), blk & 63));
+    exist = page >= 0 ? s.len - pos : 0;
+    const uint8_t* tile = tile8_at<D>(a.c, page >= 0 ? page : 0, kh, pos) + 16 * D + 16 * lane;
+#pragma unroll
+    for (int c = 0; c < C; ++c) vw[c] = *reinterpret_cast<const u32x4*>(tile + 1024 * c);
+  };
+  const auto unpack_k = [&](int blk) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      st.k[blk & 1][wave][kk][lane] = halves8<INT8, false>(kw[kk / 2][2 * (kk % 2)], kw[kk / 2][2 * (kk % 2) + 1], ks, ks);
+    if (lane == 0) st.valid[blk & 1][wave] = k_ok;
+  };
+  const auto unpack_v = [&](int blk) {
     if (exist < 16) {   // codes of keys that do not exist may be anything
       const int n = min(max(exist - 4 * g, 0), 4);
       const uint32_t keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
@@ -509,15 +529,11 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
       for (int c = 0; c < C; ++c) vw[c] &= keep;
     }
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-      x.k[wave][kk][lane] = halves8<INT8, false>(kw[kk / 2][2 * (kk % 2)], kw[kk / 2][2 * (kk % 2) + 1], ks, ks);
-#pragma unroll
     for (int n = 0; n < NF; n += 2) {
       const h8 y = halves8<INT8, false>(vw[n / 4][n % 4], vw[n / 4][n % 4 + 1], vs, vs);
-      reinterpret_cast<h4*>(&x.v[wave / 2][n][lane])[wave % 2] = h4{y[0], y[1], y[2], y[3]};
-      reinterpret_cast<h4*>(&x.v[wave / 2][n + 1][lane])[wave % 2] = h4{y[4], y[5], y[6], y[7]};
+      reinterpret_cast<h4*>(&st.v[blk & 1][wave / 2][n][lane])[wave % 2] = h4{y[0], y[1], y[2], y[3]};
+      reinterpret_cast<h4*>(&st.v[blk & 1][wave / 2][n + 1][lane])[wave % 2] = h4{y[4], y[5], y[6], y[7]};
     }
-    if (lane == 0) x.valid[wave] = ok;
   };
 
   h8 qf[U][KK];
@@ -531,7 +547,8 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
       qf[u][kk] = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
   }
   const Scores f = scores_of(a);
-  f4 acc[U][NF], sum[U];
+  f4 acc[U][NF], sum[U], y[U][T];
+  h8 pf[T / 2][U];
   float R[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -542,17 +559,17 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   }
   const h8 ones = h8(1);
 
-  const auto compute = [&](const Stage& x, int k0, auto edge_c) {
-    constexpr bool EDGE = decltype(edge_c)::value;
-    f4 y[U][T];   // scores; MOD: in units of log 2
+  // a block's scores
+  const auto score_block = [&](int blk) {
+    const auto& k = st.k[blk & 1];
     h8 kf[2][KK];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) kf[0][kk] = x.k[0][kk][lane];
+    for (int kk = 0; kk < KK; ++kk) kf[0][kk] = k[0][kk][lane];
 #pragma unroll
     for (int j = 0; j < T; ++j) {
       if (j + 1 < T) {
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[(j + 1) & 1][kk] = x.k[j + 1][kk][lane];
+        for (int kk = 0; kk < KK; ++kk) kf[(j + 1) & 1][kk] = k[j + 1][kk][lane];
       }
       __builtin_amdgcn_sched_barrier(0);  // (these loads travel beside this tile's work)
 #pragma unroll
@@ -562,34 +579,72 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int u = 0; u < U; ++u) y[u][j] = mfma16(kf[j & 1][kk], qf[u][kk], y[u][j]);
     }
-    if constexpr (MOD || EDGE) {
+  };
+  // the weights' products with the values
+  const auto add_block = [&](int blk) {
+    constexpr int N = NF / 2;
+    const auto& v = st.v[blk & 1];
+    h8 vf[2][N];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int col = c0 + 16 * u + r, qj = col / a.G, at = s.len - s.nq + qj;
-      Seen see = Seen{0, 0};
-      if (col < cols) see = seen_by(a, s, qj);
-      const int pre = col < cols ? s.pre : 0;
+    for (int n = 0; n < N; ++n) vf[0][n] = v[0][n][lane];
 #pragma unroll
-      for (int j = 0; j < T; ++j)
+    for (int i = 0; i < T; ++i) {   // half of a pair of tiles' fragments at a time
+      const int t = i / 2, half = i % 2;
+      if (i + 1 < T) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int key = k0 + 16 * j + 4 * g + e;
-          float v = y[u][j][e];
-          if constexpr (MOD) {
-            const int far = at - key;
-            v = score(f, v, slope[u], (float)(far < 0 ? -far : far));
-          }
-          if constexpr (EDGE) {
-            const bool in = x.valid[j] && ((key >= see.lo && key < see.hi) || key < pre);
-            v = in ? v : -INFINITY;
-          }
-          y[u][j][e] = v;
-        }
+        for (int n = 0; n < N; ++n) vf[(i + 1) & 1][n] = v[(i + 1) / 2][(i + 1) % 2 * N + n][lane];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          acc[u][half * N + n] = mfma16(vf[i & 1][n], pf[t][u], acc[u][half * N + n]);
+      if (half == 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum[u] = mfma16(ones, pf[t][u], sum[u]);
+      }
     }
+  };
+  // scores to weights
+  const auto weigh_block = [&](int k0, int blk) {
+    constexpr float unit = MOD ? 1.f : kLog2e;   // (MOD: scores become units of log 2)
+    const int base = k0 + 4 * g;   // this lane's keys count from here
+    uint32_t valid = 0;
+#pragma unroll
+    for (int j = 0; j < T; ++j) valid |= (uint32_t)__builtin_amdgcn_readfirstlane(st.valid[blk & 1][j]) << j;
+    if constexpr (MOD) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // the bias as for keys up to the column's position
+        const float far = slope[u] * (float)(s.len - s.nq + (c0 + 16 * u + r) / a.G - base);
+#pragma unroll
+        for (int j = 0; j < T; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            y[u][j][e] = __builtin_fmaf(slope[u], (float)(16 * j + e), score(f, y[u][j][e])) - far;
+      }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    constexpr float unit = MOD ? 1.f : kLog2e;
-    float shift[U];
+    // not all columns see all of the keys
+    if (valid != (1u << T) - 1 || k0 < all_lo || k0 + kManyKeys > all_hi) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int col = c0 + 16 * u + r, qj = col / a.G, at = s.len - s.nq + qj;
+        Seen see = Seen{0, 0};
+        if (col < cols) see = seen_by(a, s, qj);
+        const int hi = see.hi - base, lo = see.lo - base, pre = (col < cols ? s.pre : 0) - base;
+#pragma unroll
+        for (int j = 0; j < T; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int key = 16 * j + e;
+            const bool in = (valid >> j & 1) && ((key >= lo && key < hi) || key < pre);
+            if constexpr (MOD)   // (keys past it: of a prefix)
+              y[u][j][e] = __builtin_fmaf(slope[u], -2.f * (float)max(key - (at - base), 0), y[u][j][e]);
+            y[u][j][e] = in ? y[u][j][e] : -INFINITY;
+          }
+      }
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float top = -INFINITY;
@@ -598,75 +653,54 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, y[u][j][e]);
       const float Rn = fmaxf(R[u], cols_max(top) * unit);
-      const float Rs = EDGE && Rn == -INFINITY ? 0.f : Rn;
+      const float Rs = Rn == -INFINITY ? 0.f : Rn;
       const float alpha = __builtin_amdgcn_exp2f(R[u] - Rs);
       R[u] = Rn;
-      shift[u] = kPBits - Rs;
+      const float shift = kPBits - Rs;
       if (__any(alpha != 1.f)) {
         sum[u] *= alpha;
 #pragma unroll
         for (int n = 0; n < NF; ++n) acc[u][n] *= alpha;
       }
-    }
 #pragma unroll
-    for (int t = 0; t < T / 2; ++t) {
-      h8 vf[NF / 2], pf[U];
+      for (int j = 0; j < T; ++j)
 #pragma unroll
-      for (int n = 0; n < NF / 2; ++n) vf[n] = x.v[t][n][lane];
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            pf[u][4 * jj + e] =
-                (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(y[u][2 * t + jj][e], unit, shift[u]));
-        sum[u] = mfma16(ones, pf[u], sum[u]);
-      }
-#pragma unroll
-      for (int n = 0; n < NF; ++n) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) acc[u][n] = mfma16(vf[n % (NF / 2)], pf[u], acc[u][n]);
-        if (n < NF / 2) vf[n] = x.v[t][n + NF / 2][lane];
-      }
-      __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < 4; ++e)
+          pf[j / 2][u][4 * (j % 2) + e] =
+              (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(y[u][j][e], unit, shift));
     }
   };
 
+  // Per block: the one after next is asked for, the next one unpacked, the last one's products
+  // with the values and this one's scores made, and weights of these.
+  if (tid < TEAMS) lds.arrived[tid] = 0;
   if (mine > 0) {
-    fetch(0);
-    unpack(st[0]);
+    fetch_k(0);
+    unpack_k(0);
+    fetch_v(0);
+    if (mine > 1) fetch_k(1);
   }
   __syncthreads();
-  // blocks that every column of the wave sees whole, and others, in turn
-  int blk = 0;
-  const auto run = [&](auto edge_c) {
-    constexpr bool EDGE = decltype(edge_c)::value;
 #pragma unroll 1
-    for (; blk < turns; ++blk) {
-      const Stage& x = st[blk & 1];
-      const int k0 = key_of(blk), k1 = k0 + kManyKeys;
-      bool whole = false;
-      if (blk < mine) {
-        uint32_t v = 1;
-#pragma unroll
-        for (int j = 0; j < T; ++j) v &= x.valid[j];
-        whole = __builtin_amdgcn_readfirstlane(v) && ((k0 >= all_lo && k1 <= all_hi) || k1 <= s.pre);
-      }
-      if (whole == EDGE) return;
-      if (blk + 1 < mine) fetch(blk + 1);
-      if (!EDGE || (blk < mine && ((k1 > any_lo && k0 < any_hi) || (k0 < s.pre && !idle))))
-        compute(x, k0, edge_c);
-      if (blk + 1 < mine) unpack(st[(blk + 1) & 1]);
-      __syncthreads();
+  for (int i = 0; i < mine; ++i) {
+    unpack_v(i);
+    if (i + 1 < mine) {
+      unpack_k(i + 1);
+      fetch_v(i + 1);
+      if (i + 2 < mine) fetch_k(i + 2);
     }
-  };
-#pragma unroll 1
-  while (blk < turns) {
-    run(std::false_type{});
-    run(std::true_type{});
+    if (!idle) {
+      if (i > 0) add_block(i - 1);
+      score_block(i);
+      weigh_block(key_of(i), i);
+    }
+    if constexpr (TEAMS == 2)
+      team_barrier(&lds.arrived[team], i + 1);
+    else
+      __syncthreads();
   }
+  if (!idle && mine > 0) add_block(mine - 1);
+  if (TEAMS == 2) __syncthreads();   // (the buffers are read)
 
   // element e of acc[u][n]: dimension 16 n + 4 g + e of column c0 + 16 u + r.  The
   // second team's sums go to LDS (every block there is read), the first adds them.

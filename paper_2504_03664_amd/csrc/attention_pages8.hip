@@ -23,6 +23,7 @@ struct Attn8 {
   float2* part_rl;
   int64_t ldq, ldo, M;
   int H, G, max_q, max_len, window, max_prefix;
+  double per_g;               // 1 / G
   float cap;
   int few_cols;               // up to this many are attn8_few_k's, or none
   int chunk_few, chunk_many;  // keys of a split, by the sequence's columns
@@ -39,6 +40,12 @@ constexpr int kMaxSplits = 64;  // a wave's lanes, where they are joined
 constexpr float kLog2e = 1.4426950408889634f;
 // p is held times 2^14: as a half it keeps 11 bits down to 2^-28
 constexpr float kPBits = 14.f;
+
+// column / G: of numbers below 2^31, a half added, the quotient is never within 2^-18 of a
+// whole number
+__device__ __forceinline__ int query_of(const Attn8& a, int col) {
+  return (int)(((double)col + 0.5) * a.per_g);
+}
 
 // a sequence's rows [row0, row0 + nq), how many of them count (up to max_q), its keys
 // and the ones that every row sees
@@ -83,8 +90,9 @@ __device__ __forceinline__ Blocks blocks_of(const Attn8& a, const Seq8& s, int j
 }
 template <int KEYS>
 __device__ __forceinline__ int splits_of(const Attn8& a, const Seq8& s, int chunk) {
-  const int n = s.rows > 0 ? blocks_of<KEYS>(a, s, 0, s.rows - 1).n : 0;
-  return min(max(1, (int)(((int64_t)n * KEYS + chunk - 1) / chunk)), a.splits);
+  if (a.splits == 1) return 1;
+  const uint32_t n = s.rows > 0 ? blocks_of<KEYS>(a, s, 0, s.rows - 1).n : 0, per = (uint32_t)chunk / KEYS;
+  return min(max(1, (int)((n + per - 1) / per)), a.splits);
 }
 
 template <int D>
@@ -106,47 +114,10 @@ __device__ __forceinline__ float cols_sum(float x) {
   return pair_sum(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
 }
 
-// eight codes of two words -> halves; UNIT: in units of the scale
-template <bool INT8, bool UNIT>
-__device__ __forceinline__ h8 halves8(uint32_t w0, uint32_t w1, float s0, float s1) {
-  h2 p[4];
-  if constexpr (INT8) {
-    const uint32_t f0 = w0 ^ 0x80808080u, f1 = w1 ^ 0x80808080u;
-    p[0] = int8_halves<false>(f0);
-    p[1] = int8_halves<true>(f0);
-    p[2] = int8_halves<false>(f1);
-    p[3] = int8_halves<true>(f1);
-    if constexpr (!UNIT) {
-      const _Float16 a = (_Float16)s0, b = (_Float16)s1;
-      p[0] *= h2{a, a};
-      p[1] *= h2{a, a};
-      p[2] *= h2{b, b};
-      p[3] *= h2{b, b};
-    }
-  } else {
-    p[0] = e4m3_halves<false>(w0, UNIT ? 1.f : s0);
-    p[1] = e4m3_halves<true>(w0, UNIT ? 1.f : s0);
-    p[2] = e4m3_halves<false>(w1, UNIT ? 1.f : s1);
-    p[3] = e4m3_halves<true>(w1, UNIT ? 1.f : s1);
-  }
-  return h8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
-}
-
-// what becomes of scores, in units of log 2
-struct Scores {
-  float cap_in, cap_out;   // 2 log2(e) / cap, cap log2(e); 0: no cap
-};
-__device__ __forceinline__ Scores scores_of(const Attn8& a) {
-  return Scores{a.cap > 0.f ? 2.f * kLog2e / a.cap : 0.f, a.cap * kLog2e};
-}
 // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): off by a few 2^-24 of the cap, in a
-// number whose exponential is taken
-__device__ __forceinline__ float score(const Scores& f, float x) {
-  float y = x * kLog2e;
-  if (f.cap_in > 0.f)
-    y = __builtin_fmaf(-2.f * f.cap_out,
-                       __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * f.cap_in) + 1.f), f.cap_out);
-  return y;
+// number whose exponential is taken.  `in` is 2 log2(e) / cap.
+__device__ __forceinline__ float capped(float x, float cap, float in) {
+  return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * in) + 1.f), cap);
 }
 
 // result of a column: straight to o, or a partial
@@ -193,12 +164,12 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int r = lane & 15, g = lane >> 4;
 
   // this lane's column, the keys it sees, and those that all columns see
-  const int col = 16 * ct + r, qj = col / a.G, h = kh * a.G + col % a.G;
+  const int col = 16 * ct + r, qj = query_of(a, col), h = kh * a.G + col - qj * a.G;
   Seen mine = Seen{0, 0};
   if (col < cols) mine = seen_by(a, s, qj);
   const int pre = col < cols ? s.pre : 0;
   const int at = s.len - s.nq + qj;   // its position
-  const int j0 = 16 * ct / a.G, j1 = min(s.rows - 1, (16 * ct + 15) / a.G);
+  const int j0 = query_of(a, 16 * ct), j1 = min(s.rows - 1, query_of(a, 16 * ct + 15));
   const int all_lo = seen_by(a, s, j1).lo, all_hi = seen_by(a, s, j0).hi;
   const Blocks blocks = blocks_of<kBlock>(a, s, j0, j1);
   const int per = a.chunk_few / kBlock, b1 = (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per);
@@ -244,8 +215,8 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk)
     qf[kk] = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
-  const Scores f = scores_of(a);
-  const float slope = MOD && a.slopes && col < cols ? a.slopes[h] * kLog2e : 0.f;
+  const float slope = MOD && a.slopes && col < cols ? a.slopes[h] : 0.f;
+  const float cap_in = MOD && a.cap > 0.f ? 2.f * kLog2e / a.cap : 0.f;
 
   f4 acc[NF];
 #pragma unroll
@@ -266,13 +237,23 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
         d = mfma16(halves8<INT8, true>(w[2 * (kk % 2)], w[2 * (kk % 2) + 1], 1.f, 1.f), qf[kk], d);
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (MOD) {
-          const int far = at - (key0 + 16 * j + 4 * g + e);
-          y[j][e] = __builtin_fmaf(-slope, (float)(far < 0 ? -far : far), score(f, d[e] * x.ks[j]));
-        } else {
-          y[j][e] = d[e] * (x.ks[j] * kLog2e);
-        }
+      for (int e = 0; e < 4; ++e) y[j][e] = d[e] * x.ks[j];
+    }
+    if constexpr (MOD) {
+      if (a.cap > 0.f) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[j][e] = capped(y[j][e], a.cap, cap_in);
+      }
+      if (a.slopes) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int far = at - (key0 + 16 * j + 4 * g + e);
+            y[j][e] = __builtin_fmaf(-slope, (float)(far < 0 ? -far : far), y[j][e]);
+          }
       }
     }
     if (edge) {
@@ -296,7 +277,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = fmaxf(top, y[j][e]);
-    const float Rn = fmaxf(R, cols_max(top));
+    const float Rn = fmaxf(R, cols_max(top) * kLog2e);
     const float Rs = Rn == -INFINITY ? 0.f : Rn;
     const float alpha = __builtin_amdgcn_exp2f(R - Rs);
     R = Rn;
@@ -311,7 +292,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p = __builtin_amdgcn_exp2f(y[j][e] + shift);
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(y[j][e], kLog2e, shift));
         l += p;
         hi[4 * j + e] = (_Float16)p;
         lo[4 * j + e] = (_Float16)(p - (float)hi[4 * j + e]);
@@ -359,7 +340,8 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
       A = __builtin_fmaf(lds.sums[w][cr][dim], z, A);
       L = __builtin_fmaf(lds.l[w][cr], z, L);
     }
-    put<D>(a, kh * a.G + cc % a.G, s.row0 + cc / a.G, sp, ns, dim, A, Rm, L);
+    const int j = query_of(a, cc);
+    put<D>(a, kh * a.G + cc - j * a.G, s.row0 + j, sp, ns, dim, A, Rm, L);
   }
 }
 
@@ -376,28 +358,31 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 // their keys, the most first, and of a sequence the tiles with the most keys.
 struct Place8 {
   int seq, tile;
+  Seq8 s;
 };
-__device__ __forceinline__ int many_tiles(const Attn8& a, int i) {
-  const int cols = sequence(a, i).rows * a.G;
+__device__ __forceinline__ int many_tiles(const Attn8& a, const Seq8& s) {
+  const int cols = s.rows * a.G;
   return cols > a.few_cols ? (cols + kManyCols - 1) / kManyCols : 0;
 }
 __device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
   const int n = a.c.n_seq, lane = threadIdx.x & 63;
   if (n <= 64) {
-    const int tiles = lane < n ? many_tiles(a, lane) : 0, keys = tiles ? a.kv_len[lane] : 0;
+    const Seq8 s = sequence(a, min(lane, n - 1));
+    const int tiles = lane < n ? many_tiles(a, s) : 0, keys = tiles ? s.len : 0;
     int before = 0;
     for (int i = 0; i < n; ++i) {
       const int k = __builtin_amdgcn_readlane(keys, i), w = __builtin_amdgcn_readlane(tiles, i);
       before += k > keys || (k == keys && i < lane) ? w : 0;
     }
     const uint64_t hit = __ballot(t >= before && t < before + tiles);
-    if (!hit) return Place8{-1, 0};
+    if (!hit) return Place8{-1, 0, s};
     const int i = __ffsll((unsigned long long)hit) - 1;
-    return Place8{i, __builtin_amdgcn_readlane(before + tiles - 1, i) - t};
+    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i); };
+    return Place8{i, of(before + tiles - 1) - t, Seq8{of(s.row0), of(s.nq), of(s.rows), of(s.len), of(s.pre)}};
   }
   const int each = (n + 63) / 64, first = lane * each, last = min(n, first + each);
   int sum = 0;
-  for (int i = first; i < last; ++i) sum += many_tiles(a, i);
+  for (int i = first; i < last; ++i) sum += many_tiles(a, sequence(a, i));
   int end = sum;  // of this lane's tiles
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -405,12 +390,13 @@ __device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
     if (lane >= d) end += y;
   }
   const uint64_t hit = __ballot(t >= end - sum && t < end);
-  if (!hit) return Place8{-1, 0};
+  if (!hit) return Place8{-1, 0, Seq8{}};
   const int src = __ffsll((unsigned long long)hit) - 1;
   int r = t - __builtin_amdgcn_readlane(end - sum, src);
   for (int i = src * each;; ++i) {  // (ends: r is below the sum of these)
-    const int tiles = many_tiles(a, i);
-    if (r < tiles) return Place8{i, tiles - 1 - r};
+    const Seq8 s = sequence(a, i);
+    const int tiles = many_tiles(a, s);
+    if (r < tiles) return Place8{i, tiles - 1 - r, s};
     r -= tiles;
   }
 }
@@ -457,7 +443,9 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   if (place.seq < 0) return;
   const int si = __builtin_amdgcn_readfirstlane(place.seq);
   const int ct = __builtin_amdgcn_readfirstlane(place.tile);
-  const Seq8 s = sequence(a, si);
+  const auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  const Seq8 s = Seq8{uniform(place.s.row0), uniform(place.s.nq), uniform(place.s.rows),
+                      uniform(place.s.len), uniform(place.s.pre)};
   const int cols = s.rows * a.G;
   const int ns = splits_of<kManyKeys>(a, s, a.chunk_many);
   if (sp >= ns) return;
@@ -468,7 +456,8 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   Stage& st = lds.st[team];
 
   const int c0 = kManyCols * ct + 32 * wave;  // this wave's first column
-  const int j0 = kManyCols * ct / a.G, j1 = min(s.rows - 1, (kManyCols * ct + kManyCols - 1) / a.G);
+  const int j0 = query_of(a, kManyCols * ct);
+  const int j1 = min(s.rows - 1, query_of(a, kManyCols * ct + kManyCols - 1));
   const Blocks blocks = blocks_of<kManyKeys>(a, s, j0, j1);
   const int per = a.chunk_many / kManyKeys, b0 = sp * per;
   const int n_blocks = max(0, (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per) - b0);
@@ -476,7 +465,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   const int mine = (n_blocks + TEAMS - 1 - team) / TEAMS;
   const auto key_of = [&](int blk) { return kManyKeys * blocks(b0 + TEAMS * blk + team); };
   // keys that all of the wave's columns see
-  const int w0 = c0 / a.G, w1 = min(s.rows - 1, (c0 + 31) / a.G);
+  const int w0 = query_of(a, c0), w1 = min(s.rows - 1, query_of(a, c0 + 31));
   const bool idle = c0 >= cols;
   const int all_lo = idle ? 0 : seen_by(a, s, w1).lo, all_hi = idle ? 0 : seen_by(a, s, w0).hi;
 
@@ -540,13 +529,13 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   float slope[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int col = c0 + 16 * u + r, qj = col / a.G, h = kh * a.G + col % a.G;
-    slope[u] = MOD && a.slopes && col < cols ? a.slopes[h] * kLog2e : 0.f;
+    const int col = c0 + 16 * u + r, qj = query_of(a, col), h = kh * a.G + col - qj * a.G;
+    slope[u] = MOD && a.slopes && col < cols ? a.slopes[h] : 0.f;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
       qf[u][kk] = col < cols ? load_q<D>(a, s.row0 + qj, h, 32 * kk + 8 * g) : zero_h8();
   }
-  const Scores f = scores_of(a);
+  const float cap_in = MOD && a.cap > 0.f ? 2.f * kLog2e / a.cap : 0.f;
   f4 acc[U][NF], sum[U], y[U][T];
   h8 pf[T / 2][U];
   float R[U];
@@ -608,28 +597,39 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   };
   // scores to weights
   const auto weigh_block = [&](int k0, int blk) {
-    constexpr float unit = MOD ? 1.f : kLog2e;   // (MOD: scores become units of log 2)
     const int base = k0 + 4 * g;   // this lane's keys count from here
     uint32_t valid = 0;
 #pragma unroll
     for (int j = 0; j < T; ++j) valid |= (uint32_t)__builtin_amdgcn_readfirstlane(st.valid[blk & 1][j]) << j;
+    // what is to be taken from this lane's scores: the bias of a key at `base`, as for keys up
+    // to the column's position
+    float less[U] = {};
     if constexpr (MOD) {
+      if (a.cap > 0.f) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        // the bias as for keys up to the column's position
-        const float far = slope[u] * (float)(s.len - s.nq + (c0 + 16 * u + r) / a.G - base);
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < T; ++j)
+          for (int j = 0; j < T; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            y[u][j][e] = __builtin_fmaf(slope[u], (float)(16 * j + e), score(f, y[u][j][e])) - far;
+            for (int e = 0; e < 4; ++e) y[u][j][e] = capped(y[u][j][e], a.cap, cap_in);
+      }
+      if (a.slopes) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          less[u] = slope[u] * (float)(s.len - s.nq + query_of(a, c0 + 16 * u + r) - base);
+#pragma unroll
+          for (int j = 0; j < T; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              y[u][j][e] = __builtin_fmaf(slope[u], (float)(16 * j + e), y[u][j][e]);
+        }
       }
     }
     // not all columns see all of the keys
     if (valid != (1u << T) - 1 || k0 < all_lo || k0 + kManyKeys > all_hi) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int col = c0 + 16 * u + r, qj = col / a.G, at = s.len - s.nq + qj;
+        const int col = c0 + 16 * u + r, qj = query_of(a, col), at = s.len - s.nq + qj;
         Seen see = Seen{0, 0};
         if (col < cols) see = seen_by(a, s, qj);
         const int hi = see.hi - base, lo = see.lo - base, pre = (col < cols ? s.pre : 0) - base;
@@ -652,11 +652,11 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
       for (int j = 0; j < T; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, y[u][j][e]);
-      const float Rn = fmaxf(R[u], cols_max(top) * unit);
+      const float Rn = fmaxf(R[u], cols_max(top - less[u]) * kLog2e);
       const float Rs = Rn == -INFINITY ? 0.f : Rn;
       const float alpha = __builtin_amdgcn_exp2f(R[u] - Rs);
       R[u] = Rn;
-      const float shift = kPBits - Rs;
+      const float shift = __builtin_fmaf(less[u], -kLog2e, kPBits - Rs);
       if (__any(alpha != 1.f)) {
         sum[u] *= alpha;
 #pragma unroll
@@ -667,7 +667,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           pf[j / 2][u][4 * (j % 2) + e] =
-              (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(y[u][j][e], unit, shift));
+              (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(y[u][j][e], kLog2e, shift));
     }
   };
 
@@ -739,7 +739,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
     const int col = c0 + 16 * u + r;
     const float L = l[u];
     if (col >= cols) continue;
-    const int m = s.row0 + col / a.G, h = kh * a.G + col % a.G;
+    const int qj = query_of(a, col), m = s.row0 + qj, h = kh * a.G + col - qj * a.G;
     if (ns == 1) {
       const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
       uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D;
@@ -858,7 +858,7 @@ static Plan8 plan_attn8(const pipo_kv8_pages* c, const pipo_attn_scores* f, int 
     p.chunk_few = chunk_of(few, 1, kBlock);
     p.chunk_many = chunk_of(many, 1, kManyKeys);
   }
-  p.teams = tiles > 3 * kCUs ? 1 : 2;
+  p.teams = tiles <= kCUs || (tiles <= 2 * kCUs && many > 2048) ? 2 : 1;
   p.splits_few = (int)std::max<int64_t>(1, (few + p.chunk_few - 1) / p.chunk_few);
   p.splits_many = (int)std::max<int64_t>(1, (many + p.chunk_many - 1) / p.chunk_many);
   return p;
@@ -962,6 +962,7 @@ pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* c, int32_t layer, const
   a.M = M;
   a.H = n_heads;
   a.G = n_heads / c->n_kv_heads;
+  a.per_g = 1.0 / a.G;
   a.max_q = (int)std::min<int64_t>(max_q, M);
   a.max_len = max_len;
   Plan8 p = plan_attn8(c, f, n_heads, M, a.max_q, max_len);

@@ -71,6 +71,32 @@ __device__ __forceinline__ h2 int8_halves(uint32_t w_flipped) {  // w ^ 0x808080
   return __builtin_bit_cast(h2, u) - h2{(_Float16)1152.f, (_Float16)1152.f};
 }
 
+// eight codes of two words -> halves; UNIT: in units of the scale
+template <bool INT8, bool UNIT>
+__device__ __forceinline__ h8 halves8(uint32_t w0, uint32_t w1, float s0, float s1) {
+  h2 p[4];
+  if constexpr (INT8) {
+    const uint32_t f0 = w0 ^ 0x80808080u, f1 = w1 ^ 0x80808080u;
+    p[0] = int8_halves<false>(f0);
+    p[1] = int8_halves<true>(f0);
+    p[2] = int8_halves<false>(f1);
+    p[3] = int8_halves<true>(f1);
+    if constexpr (!UNIT) {
+      const _Float16 a = (_Float16)s0, b = (_Float16)s1;
+      p[0] *= h2{a, a};
+      p[1] *= h2{a, a};
+      p[2] *= h2{b, b};
+      p[3] *= h2{b, b};
+    }
+  } else {
+    p[0] = e4m3_halves<false>(w0, UNIT ? 1.f : s0);
+    p[1] = e4m3_halves<true>(w0, UNIT ? 1.f : s0);
+    p[2] = e4m3_halves<false>(w1, UNIT ? 1.f : s1);
+    p[3] = e4m3_halves<true>(w1, UNIT ? 1.f : s1);
+  }
+  return h8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
+}
+
 pipo_status check_pages8(const char* what, const pipo_kv8_pages* c, int32_t layer, Pages8* v);
 
 }  // namespace pipo

@@ -3,7 +3,7 @@
 //
 //   pages8_append_k: a wave for each tile of 16 positions that gets rows, head, and K
 //                    or V: it alone holds what decides the tile's scale.
-//   pages8_read_k:   slots -> fp16 rows, a thread on eight elements.
+//   pages8_read_k:   slots -> fp16 rows, a thread on 32 elements of two heads.
 // With scales that are powers of two every product here is exact; only the
 // conversions to codes round.
 #include "kvpages8.h"
@@ -67,8 +67,11 @@ __device__ __forceinline__ void clamp8(h8& x, uint32_t& top) {
     for (int j = 0; j < 8; ++j) {
       const float f = (float)x[j];
       x[j] = (_Float16)(f == f ? fminf(fmaxf(f, -kKv8Clamp), kKv8Clamp) : 0.f);
-      t[0] = max(t[0], (uint16_t)(__builtin_bit_cast(uint16_t, x[j]) & 0x7FFF));
     }
+    w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      t = __builtin_elementwise_max(t, __builtin_bit_cast(us2, w[j] & 0x7FFF7FFFu));
   }
   top = max(top, (uint32_t)max(t[0], t[1]));
 }
@@ -112,6 +115,19 @@ __device__ __forceinline__ uint32_t transpose4(uint32_t w, int lane) {
   w = lane & 1 ? __builtin_amdgcn_perm(w, o, 0x07030501u) : __builtin_amdgcn_perm(o, w, 0x06020400u);
   const uint32_t p = quad_move<0x4E>(w);
   return lane & 2 ? __builtin_amdgcn_perm(w, p, 0x07060302u) : __builtin_amdgcn_perm(p, w, 0x05040100u);
+}
+
+// eight codes as halves to a row
+template <bool INT8, bool VEC>
+__device__ __forceinline__ void store8(uint16_t* dst, uint32_t w0, uint32_t w1, float scale) {
+  const h8 x = halves8<INT8, false>(w0, w1, scale, scale);
+  if constexpr (VEC) {
+    *reinterpret_cast<u32x4*>(dst) = __builtin_bit_cast(u32x4, x);
+  } else {
+    const u32x4 y = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dst[j] = (uint16_t)(y[j / 2] >> (16 * (j & 1)));
+  }
 }
 
 template <bool VEC>
@@ -233,57 +249,81 @@ __global__ __launch_bounds__(256) void pages8_append_k(Rows8 a) {
   if (lane == 0) *scale_at = power(e);
 }
 
-// a thread on eight elements of a row's head (values behind keys)
+// A thread on 32 elements of a row's heads h0, h0 + step .. (values behind keys), D / 32
+// threads a head, sixteen rows of a head side by side: rows that are consecutive positions,
+// as of a prefix, then read the same words of values, a byte each of 16 bytes that a
+// thread loads, out of the first-level cache (byte by byte, eight a thread, 70 us where this
+// takes 46: eight prompts of 512
+// rows, 56 heads of 128; stored past the L2, in its pieces of 32 bytes, 96).
+constexpr int kReadHeads = 2;
+__host__ __device__ constexpr int64_t read_step(int Hkv) {
+  return (2 * (int64_t)Hkv + kReadHeads - 1) / kReadHeads;
+}
 template <int D, bool INT8, bool VEC>
 __global__ __launch_bounds__(256) void pages8_read_k(Pages8 c, const int32_t* __restrict__ seq,
                                                      const int32_t* __restrict__ pos,
                                                      uint16_t* __restrict__ k, int64_t ldk,
                                                      uint16_t* __restrict__ v, int64_t ldv, int64_t M) {
-  constexpr int LANES = D / 8;
+  constexpr int UN = D / 32;
   const int64_t e = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-  const uint32_t per_row = 2 * c.Hkv * LANES;
-  const int64_t m = e / per_row;
+  const uint32_t step = (uint32_t)read_step(c.Hkv), per_group = step * 16 * UN;
+  const int64_t group = e < ((int64_t)1 << 32) ? (uint32_t)e / per_group : e / per_group;
+  const uint32_t r = (uint32_t)(e - group * per_group);
+  const int64_t m = 16 * group + r / UN % 16;
   if (m >= M) return;
-  const int x = (int)(e - m * per_row) % LANES, hv = (int)(e - m * per_row) / LANES;
-  const bool value = hv >= c.Hkv;
-  const int head = value ? hv - c.Hkv : hv;
+  const int unit = r % UN, cc = unit / 2, h = unit % 2;
   const int i = seq[m], p = pos[m];
   if (i < 0 || i >= c.n_seq || p < 0 || (p >> c.ps_log2) >= c.stride) return;
   const int page = c.table[i * c.stride + (p >> c.ps_log2)];
   if (page < 0 || page >= c.n_pages) return;
   const int key = p & 15;
-  const uint8_t* tile = tile8_at<D>(c, page, head, p);
-  const float scale = scales8_at(c, page, head, p)[value ? 1 : 0];
-  uint32_t w[2];
-  if (!value) {
-    const u32x2 y = *reinterpret_cast<const u32x2*>(tile + 1024 * (x / 8) + 16 * (key + 16 * (x % 4)) +
-                                                    8 * (x / 4 % 2));
-    w[0] = y[0];
-    w[1] = y[1];
-  } else {
-    const uint8_t* at =
-        tile + 16 * D + 1024 * (x / 8) + 16 * (8 * (x % 2) + 16 * (key >> 2)) + 4 * (x / 2 % 4) + (key & 3);
+  float scale[kReadHeads];
+  u32x4 w[kReadHeads][8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      w[j] = at[64 * j] | (uint32_t)at[64 * j + 16] << 8 | (uint32_t)at[64 * j + 32] << 16 |
-             (uint32_t)at[64 * j + 48] << 24;
+  for (int t = 0; t < kReadHeads; ++t) {
+    const int hv = (int)(r / (16 * UN) + t * step);
+    if (hv >= 2 * c.Hkv) break;
+    const bool value = hv >= c.Hkv;
+    const int head = value ? hv - c.Hkv : hv;
+    const uint8_t* tile = tile8_at<D>(c, page, head, p) + 1024 * cc;
+    scale[t] = scales8_at(c, page, head, p)[value ? 1 : 0];
+    if (value) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        w[t][j] = *reinterpret_cast<const u32x4*>(tile + 16 * D + 16 * (8 * h + j + 16 * (key >> 2)));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        w[t][j] = *reinterpret_cast<const u32x4*>(tile + 16 * (key + 16 * (2 * h + j)));
+    }
   }
-  uint16_t out[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t y = w[j / 4] >> (8 * (j % 4));
-    const float f = INT8 ? (float)(int8_t)y : (float)e4m3_halves<false>(y, 1.f)[0];
-    out[j] = f2h(f * scale);
-  }
-  uint16_t* dst = (value ? v + m * ldv : k + m * ldk) + (int64_t)head * D + 8 * x;
-  if constexpr (VEC) {
-    u32x4 o;
+  for (int t = 0; t < kReadHeads; ++t) {
+    const int hv = (int)(r / (16 * UN) + t * step);
+    if (hv >= 2 * c.Hkv) break;
+    const bool value = hv >= c.Hkv;
+    const int head = value ? hv - c.Hkv : hv;
+    uint16_t* dst = (value ? v + m * ldv : k + m * ldk) + (int64_t)head * D + 64 * cc;
+    if (value) {   // the key's byte of each word: words of four dimensions
+      const uint32_t two = 0x0C0C0400u + 0x0101u * (key & 3);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = (uint32_t)out[2 * j] | (uint32_t)out[2 * j + 1] << 16;
-    *reinterpret_cast<u32x4*>(dst) = o;
-  } else {
+      for (int n = 0; n < 4; ++n) {
+        uint32_t y[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dst[j] = out[j];
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t lo = __builtin_amdgcn_perm(w[t][4 * j + 1][n], w[t][4 * j][n], two);
+          const uint32_t hi = __builtin_amdgcn_perm(w[t][4 * j + 3][n], w[t][4 * j + 2][n], two);
+          y[j] = lo | hi << 16;
+        }
+        store8<INT8, VEC>(dst + 16 * n + 8 * h, y[0], y[1], scale[t]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          store8<INT8, VEC>(dst + 32 * n + 8 * (2 * h + j), w[t][j][2 * n], w[t][j][2 * n + 1], scale[t]);
+    }
   }
 }
 
@@ -416,9 +456,9 @@ pipo_status pipo_op_kv8_pages_read(const pipo_kv8_pages* c, int32_t layer, const
   PIPO_TRY(check_pages8("kv8_pages_read", c, layer, &view));
   PIPO_TRY(check_rows8("kv8_pages_read", c, seq, pos, k, ldk, v, ldv, M));
   if (M == 0) return PIPO_OK;
-  const int64_t per_row = 2 * (int64_t)c->n_kv_heads * (c->head_dim / 8);
-  const int64_t blocks = M >= ((int64_t)1 << 62) / per_row ? INT64_MAX : (M * per_row + 255) / 256;
-  if (blocks >= ((int64_t)1 << 37) || per_row >= ((int64_t)1 << 31)) {
+  const int64_t per_group = read_step(c->n_kv_heads) * (c->head_dim / 2), groups = (M + 15) / 16;
+  const int64_t blocks = (groups * per_group + 255) / 256;
+  if (per_group >= ((int64_t)1 << 31) || blocks >= ((int64_t)1 << 37)) {
     set_error("kv8_pages_read: %lld rows of %d heads", (long long)M, c->n_kv_heads);
     return PIPO_ERR_UNSUPPORTED;
   }

@@ -261,6 +261,20 @@ def test_append_by_pieces(D, ps, fmt):
 
 
 @BOTH
+def test_append_of_infinities_anywhere(fmt):
+    """One element out of range or not a number, at every place of a row and a block."""
+    rng = np.random.default_rng(20)
+    n, bad = 128, [np.inf, -np.inf, np.nan, 60000, -65504]
+    c = Cache([n], 1, 128, 32, fmt, rng)
+    k, v = (rng.standard_normal((n, 128)).astype(np.float16) for _ in "kv")
+    for i in range(0, n, 8):       # some blocks have one, some more
+        k[i + i // 8 % 8, (37 * i) % 128] = bad[i // 8 % 5]
+        v[i // 2, (i + 53) % 128] = bad[(i // 8 + 1) % 5]
+    c.append([k], [v])
+    c.check_all()
+
+
+@BOTH
 def test_append_extremes(fmt):
     """The largest and least scales; a begun block whose scale is above what new rows need."""
     rng = np.random.default_rng(8)

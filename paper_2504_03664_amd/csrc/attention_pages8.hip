@@ -156,6 +156,13 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int kh = blockIdx.x % a.c.Hkv, si = blockIdx.x / a.c.Hkv, sp = blockIdx.y, ct = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int per = a.chunk_few / kBlock;
+  const int32_t* table = a.c.table + si * a.c.stride;
+  // (without a window a split's blocks do not depend on the lengths, and the first pages are
+  // read beside these)
+  int pages = -1;
+  const int64_t ahead = kBlock * ((int64_t)sp * per + wave + (lane >> 1) * W) + 16 * (lane & 1);
+  if (a.window <= 0 && ahead < a.max_len) pages = table[ahead >> a.c.ps_log2];
   const Seq8 s = sequence(a, si);
   const int cols = s.rows * a.G;
   if (16 * ct >= cols || cols > a.few_cols) return;
@@ -172,27 +179,25 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
   const int j0 = query_of(a, 16 * ct), j1 = min(s.rows - 1, query_of(a, 16 * ct + 15));
   const int all_lo = seen_by(a, s, j1).lo, all_hi = seen_by(a, s, j0).hi;
   const Blocks blocks = blocks_of<kBlock>(a, s, j0, j1);
-  const int per = a.chunk_few / kBlock, b1 = (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per);
+  const int b1 = (int)min((int64_t)blocks.n, (int64_t)(sp + 1) * per);
   int b = sp * per + wave;
   const auto key_of = [&](int b) { return kBlock * blocks(b); };
 
   // lane 2 i + j holds the page and the scales of tile j of the wave's i-th block, 32
   // blocks at a time
-  const int32_t* table = a.c.table + si * a.c.stride;
-  int pages = -1, turn = 32;
+  int turn = 32;
+  bool known = a.window <= 0;
   float2 scales = make_float2(1.f, 1.f);
   const auto load = [&](Block8<D>& x, int b) {
     if (turn == 32) {
       turn = 0;
       const int64_t mb = (int64_t)b + (lane >> 1) * W;
-      pages = -1;
+      const int pos = mb < b1 ? key_of((int)mb) + 16 * (lane & 1) : INT32_MAX;
+      if (!known) pages = pos < s.len ? table[pos >> a.c.ps_log2] : -1;
+      if (pos >= s.len || pages < 0 || pages >= a.c.n_pages) pages = -1;
       scales = make_float2(1.f, 1.f);
-      if (mb < b1) {
-        const int pos = key_of((int)mb) + 16 * (lane & 1);
-        if (pos < s.len) pages = table[pos >> a.c.ps_log2];
-        if (pages < 0 || pages >= a.c.n_pages) pages = -1;
-        if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
-      }
+      if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
+      known = false;
     }
     const int key = key_of(b);
 #pragma unroll
@@ -781,19 +786,29 @@ __device__ __forceinline__ int seq_of_row(const Attn8& a, int m) {
   return lo < a.c.n_seq ? lo : -1;
 }
 
-// Adds the splits of a row's head, in order: a wave for each head, D / 64 dimensions a lane.
-template <int D>
+// Adds the splits of a row's head, in order: WAVES waves take them by turns, each asking for
+// EACH at once, D / 64 dimensions a lane, and are added in order.  What there may be is
+// asked for before the row's sequence is known.
+template <int D, int WAVES, int EACH>
 __global__ __launch_bounds__(256) void attn8_merge_k(Attn8 a) {
-  constexpr int N = D / 64;
-  const int m = blockIdx.x, h = 4 * blockIdx.y + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  constexpr int N = D / 64, HEADS = 4 / WAVES;
+  typedef float fn __attribute__((ext_vector_type(N)));
+  __shared__ fn sums[4][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % WAVES;
+  const int m = blockIdx.x, h = HEADS * blockIdx.y + wave / WAVES, lane = threadIdx.x & 63;
+  const int64_t at = ((int64_t)m * a.H + min(h, a.H - 1)) * a.splits;
+  fn x[EACH];
+#pragma unroll
+  for (int j = 0; j < EACH; ++j)
+    x[j] = *reinterpret_cast<const fn*>(a.part + (at + min(part + j * WAVES, a.splits - 1)) * D + N * lane);
+  float2 rl = a.part_rl[at + min(lane, a.splits - 1)];
   const int i = seq_of_row(a, m);
-  if (i < 0 || h >= a.H) return;
+  if (i < 0) return;
   const Seq8 s = sequence(a, i);
   const int ns = s.rows * a.G <= a.few_cols ? splits_of<kBlock>(a, s, a.chunk_few)
                                             : splits_of<kManyKeys>(a, s, a.chunk_many);
   if (ns == 1 || m - s.row0 >= s.rows) return;
-  const int64_t at = ((int64_t)m * a.H + h) * a.splits;
-  const float2 rl = lane < ns ? a.part_rl[at + lane] : make_float2(-INFINITY, 0.f);
+  if (lane >= ns) rl = make_float2(-INFINITY, 0.f);
   float R = rl.x, w = 0.f;
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) R = fmaxf(R, wave_shfl_xor(R, d));
@@ -801,15 +816,25 @@ __global__ __launch_bounds__(256) void attn8_merge_k(Attn8 a) {
   float L = rl.y * w;
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) L += wave_shfl_xor(L, d);
-  float A[N] = {};
-  for (int j = 0; j < ns; ++j) {
-    const float z = __shfl(w, j, 64);
+  fn A = {};
 #pragma unroll
-    for (int n = 0; n < N; ++n) A[n] = __builtin_fmaf(a.part[(at + j) * D + 64 * n + lane], z, A[n]);
+  for (int j = 0; j < EACH; ++j) {
+    const float z = __shfl(w, min(part + j * WAVES, 63), 64);
+    if (part + j * WAVES < ns) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) A[n] = __builtin_fmaf(x[j][n], z, A[n]);
+    }
   }
-  uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D;
+  if constexpr (WAVES > 1) {
+    sums[wave][lane] = A;
+    __syncthreads();
+    if (part > 0) return;
+    for (int k = 1; k < WAVES; ++k) A += sums[wave + k][lane];
+  }
+  if (h >= a.H) return;
+  uint16_t* o = a.o + (int64_t)m * a.ldo + (int64_t)h * D + N * lane;
 #pragma unroll
-  for (int n = 0; n < N; ++n) o[64 * n + lane] = f2h(L > 0.f ? A[n] / L : (L == L ? 0.f : L));
+  for (int n = 0; n < N; ++n) o[n] = f2h(L > 0.f ? A[n] / L : (L == L ? 0.f : L));
 }
 
 static int64_t col_tiles(int64_t max_q, int G, int tile) { return (max_q * G + tile - 1) / tile; }
@@ -910,8 +935,12 @@ static void launch_attn8(const Attn8& a, const Plan8& p, hipStream_t st) {
     else
       launch(attn8_many_k<D, INT8, MOD, 1>, g, dim3(256), 0, st, a);
   }
-  if (p.splits() > 1)
-    launch(attn8_merge_k<D>, dim3((unsigned)a.M, (unsigned)((a.H + 3) / 4)), dim3(256), 0, st, a);
+  constexpr int kSmallMerge = 8;
+  if (p.splits() > kSmallMerge)
+    launch(attn8_merge_k<D, 4, kMaxSplits / 4>, dim3((unsigned)a.M, (unsigned)a.H), dim3(256), 0, st, a);
+  else if (p.splits() > 1)
+    launch(attn8_merge_k<D, 1, kSmallMerge>, dim3((unsigned)a.M, (unsigned)((a.H + 3) / 4)), dim3(256), 0,
+           st, a);
 }
 
 }  // namespace pipo

@@ -359,8 +359,10 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 // rounded ones that are added up to divide by.
 
 // The t-th column tile of the launch: its sequence (-1: none) and which of the
-// sequence's tiles.  Only sequences of many columns have tiles.  Up to 64 sequences go by
-// their keys, the most first, and of a sequence the tiles with the most keys.
+// sequence's tiles.  Only sequences of many columns have tiles.  The tiles of up to 64
+// sequences go by the keys that they may see, the most first: those that start when the
+// last ones end are short (8 prompts of 512 rows, 16 tiles each of 1 to 8 blocks: 66 us
+// sequence by sequence, 55 us so).
 struct Place8 {
   int seq, tile;
   Seq8 s;
@@ -369,21 +371,56 @@ __device__ __forceinline__ int many_tiles(const Attn8& a, const Seq8& s) {
   const int cols = s.rows * a.G;
   return cols > a.few_cols ? (cols + kManyCols - 1) / kManyCols : 0;
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_0(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+// sums of this lane's number and those of the lanes before it
+__device__ __forceinline__ int lanes_scan(int x) {
+  x += dpp_or_0<0x111, 0xF>(x);  // row_shr by 1, 2, 4, 8
+  x += dpp_or_0<0x112, 0xF>(x);
+  x += dpp_or_0<0x114, 0xF>(x);
+  x += dpp_or_0<0x118, 0xF>(x);
+  x += dpp_or_0<0x142, 0xA>(x);  // row_bcast of lane 15, then of lane 31
+  x += dpp_or_0<0x143, 0xC>(x);
+  return x;
+}
+__device__ __forceinline__ int lanes_max(int x) {  // of numbers from 0 up
+  x = max(x, dpp_or_0<0x111, 0xF>(x));
+  x = max(x, dpp_or_0<0x112, 0xF>(x));
+  x = max(x, dpp_or_0<0x114, 0xF>(x));
+  x = max(x, dpp_or_0<0x118, 0xF>(x));
+  x = max(x, dpp_or_0<0x142, 0xA>(x));
+  x = max(x, dpp_or_0<0x143, 0xC>(x));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
   const int n = a.c.n_seq, lane = threadIdx.x & 63;
   if (n <= 64) {
     const Seq8 s = sequence(a, min(lane, n - 1));
-    const int tiles = lane < n ? many_tiles(a, s) : 0, keys = tiles ? s.len : 0;
-    int before = 0;
-    for (int i = 0; i < n; ++i) {
-      const int k = __builtin_amdgcn_readlane(keys, i), w = __builtin_amdgcn_readlane(tiles, i);
-      before += k > keys || (k == keys && i < lane) ? w : 0;
+    const int tiles = lane < n ? many_tiles(a, s) : 0, keys = tiles ? (s.len + kManyKeys - 1) / kManyKeys : 0;
+    // of a sequence, tiles that see more than about k blocks, where its last sees them all:
+    // fewer with each k, and all below 0
+    const float each = (float)kManyKeys * a.G / kManyCols;
+    const auto above = [&](int k) {
+      return k < 0 ? tiles : (int)fminf(fmaxf((float)(keys - k) * each, 0.f), (float)tiles);
+    };
+    // the least k with up to t tiles above it: tile t sees k blocks
+    int k = 0, most = lanes_max(keys);
+    while (k < most) {
+      const int mid = (k + most) / 2;
+      if (__builtin_amdgcn_readlane(lanes_scan(above(mid)), 63) <= t) most = mid;
+      else k = mid + 1;
     }
-    const uint64_t hit = __ballot(t >= before && t < before + tiles);
+    const int longer = above(k), like = above(k - 1) - longer;
+    const int rest = t - __builtin_amdgcn_readlane(lanes_scan(longer), 63);
+    const int end = lanes_scan(like);
+    const uint64_t hit = __ballot(rest >= end - like && rest < end);
     if (!hit) return Place8{-1, 0, s};
     const int i = __ffsll((unsigned long long)hit) - 1;
     const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i); };
-    return Place8{i, of(before + tiles - 1) - t, Seq8{of(s.row0), of(s.nq), of(s.rows), of(s.len), of(s.pre)}};
+    return Place8{i, of(tiles - 1 - longer + end - like) - rest,
+                  Seq8{of(s.row0), of(s.nq), of(s.rows), of(s.len), of(s.pre)}};
   }
   const int each = (n + 63) / 64, first = lane * each, last = min(n, first + each);
   int sum = 0;
@@ -530,6 +567,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
     }
   };
 
+  if (mine > 0) fetch_k(0);
   h8 qf[U][KK];
   float slope[U];
 #pragma unroll
@@ -680,7 +718,6 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   // with the values and this one's scores made, and weights of these.
   if (tid < TEAMS) lds.arrived[tid] = 0;
   if (mine > 0) {
-    fetch_k(0);
     unpack_k(0);
     fetch_v(0);
     if (mine > 1) fetch_k(1);

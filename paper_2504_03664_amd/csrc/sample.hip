@@ -87,35 +87,56 @@ __device__ __forceinline__ int bin_below(const Spot& s, float x, float m, double
   const double d = bm - s.b;
   return x == m ? 0 : x > -INFINITY && d < (double)kBins ? (int)d : kBins;   // (NaN: not)
 }
+// exp(d) 2^kUnitBits, d = (f / 2^32 - 1/2) / 8: 1 + d in whole numbers, and here d^2 / 2 ..
+// d^5 / 120 in fp32 (z = d 2^18, whose square is in units), of which the last step is 2^-33
+// of the weight, and what is left out 2^-33.5
+__device__ __forceinline__ uint32_t bend_of(uint32_t f) {
+  static_assert(kUnitBits == 36, "z's units");
+  const float z = (float)(int)(f ^ 0x80000000u) * 0x1p-17f;
+  float q = __builtin_fmaf(z, 0x1p-54f / 120.f, 0x1p-36f / 24.f);
+  q = __builtin_fmaf(q, z, 0x1p-18f / 6.f);
+  q = __builtin_fmaf(q, z, 0.5f);
+  return (uint32_t)(q * (z * z));
+}
+constexpr uint32_t kOneUpper = (1u << (kUnitBits - 32)) - 1;   // 1 - 1/16 of the weight
+__device__ __forceinline__ u64 units_of(uint32_t f) {
+  return ((u64)kOneUpper << 32 | bend_of(f)) + ((u64)f << 1);
+}
+
 // The same from the two words of one sum, whose upper words differ as bins do; what is
 // not `on` is for numbers of which hardly two are in one bin.
 struct Fast {
   bool on;
   int top;
-  float low;
   double rate;
   __device__ __forceinline__ Fast(float m, double r, double bm) : rate(r) {
     on = __builtin_fabs(bm) < kMagicMost - 1024.0 && rate > 0.0;
     top = (int)(__builtin_bit_cast(uint64_t, __builtin_fma((double)m, rate, kMagic)) >> 32);
-    low = (float)((double)m - 300.0 / rate);   // (past the last bin)
   }
-  // (not below kBins: not counted; NaN neither)
+  // (not below kBins: not counted; NaN neither.  Of sums below 2^20, which have other
+  // exponents or the sign bit, the upper word is farther from `top` than that.)
+  __device__ __forceinline__ uint32_t bin(float x, u64& sum) const {
+    sum = __builtin_bit_cast(u64, __builtin_fma((double)x, rate, kMagic));
+    return (uint32_t)(top - (int)(sum >> 32));
+  }
   __device__ __forceinline__ uint32_t bin(float x, uint32_t& f) const {
-    const uint64_t s = __builtin_bit_cast(uint64_t, __builtin_fma((double)fmaxf(x, low), rate, kMagic));
-    f = (uint32_t)s;
-    return (uint32_t)(top - (int)(s >> 32));
+    u64 sum;
+    const uint32_t r = bin(x, sum);
+    f = (uint32_t)sum;
+    return r;
+  }
+  // units of a number of bin r, and one of its count: the sum's upper word, top - r, is
+  // taken off where it counts twice, which is cheaper than to clear it (the compiler
+  // would: hence the instructions)
+  __device__ __forceinline__ u64 counted(u64 sum, uint32_t r) const {
+    const uint32_t first = kOneUpper + (1u << (kCountShift - 32)) - 2u * (uint32_t)top;
+    uint32_t upper;
+    asm("v_lshl_add_u32 %0, %1, 1, %2" : "=v"(upper) : "v"(r), "v"(first));
+    u64 w = (u64)upper << 32 | bend_of((uint32_t)sum);
+    asm("v_lshl_add_u64 %0, %1, 1, %0" : "+v"(w) : "v"(sum));
+    return w;
   }
 };
-// exp(d) 2^kUnitBits, d = (f / 2^32 - 1/2) / 8: 1 + d in whole numbers, d^2 / 2 .. d^5 / 120 in
-// fp32, of which the last step is 2^-33 of the weight, and what is left out 2^-33.5
-__device__ __forceinline__ u64 units_of(uint32_t f) {
-  const float d = (float)(int)(f - 0x80000000u) * 0x1p-35f;
-  float q = __builtin_fmaf(d, 1.f / 120.f, 1.f / 24.f);
-  q = __builtin_fmaf(q, d, 1.f / 6.f);
-  q = __builtin_fmaf(q, d, 0.5f);
-  q = q * (d * d) * 0x1p36f;
-  return (1ull << kUnitBits) - (1ull << 32) + ((u64)f << 1) + (uint32_t)q;
-}
 
 // keys that rise as logits fall (-0 as 0), and back
 __device__ __forceinline__ uint32_t falling(float x) {
@@ -191,11 +212,19 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
   const double bm = spot_of(m, rate).b;
   const Fast fast(m, rate, bm);
   if (fast.on) {
+    constexpr int N = 4;   // whose steps fill each other's waits
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      uint32_t f;
-      const uint32_t r = fast.bin(v[e], f);
-      if (r < kBins) atomicAdd(&bins[r][lane & 3], units_of(f) + (1ull << kCountShift));
+    for (int e = 0; e < E; e += N) {
+      uint32_t r[N];
+      u64 w[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) r[j] = fast.bin(v[e + j], w[j]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = fast.counted(w[j], r[j]);
+      asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));   // (not in the branches)
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (r[j] < kBins) atomicAdd(&bins[r[j]][lane & 3], w[j]);
     }
   } else {
     for (int i = tid; i < n; i += 256) {

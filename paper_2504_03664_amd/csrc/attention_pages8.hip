@@ -371,20 +371,6 @@ __device__ __forceinline__ int many_tiles(const Attn8& a, const Seq8& s) {
   const int cols = s.rows * a.G;
   return cols > a.few_cols ? (cols + kManyCols - 1) / kManyCols : 0;
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_or_0(int x) {
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
-}
-// sums of this lane's number and those of the lanes before it
-__device__ __forceinline__ int lanes_scan(int x) {
-  x += dpp_or_0<0x111, 0xF>(x);  // row_shr by 1, 2, 4, 8
-  x += dpp_or_0<0x112, 0xF>(x);
-  x += dpp_or_0<0x114, 0xF>(x);
-  x += dpp_or_0<0x118, 0xF>(x);
-  x += dpp_or_0<0x142, 0xA>(x);  // row_bcast of lane 15, then of lane 31
-  x += dpp_or_0<0x143, 0xC>(x);
-  return x;
-}
 __device__ __forceinline__ int lanes_max(int x) {  // of numbers from 0 up
   x = max(x, dpp_or_0<0x111, 0xF>(x));
   x = max(x, dpp_or_0<0x112, 0xF>(x));
@@ -409,12 +395,12 @@ __device__ __forceinline__ Place8 place_of(const Attn8& a, int t) {
     int k = 0, most = lanes_max(keys);
     while (k < most) {
       const int mid = (k + most) / 2;
-      if (__builtin_amdgcn_readlane(lanes_scan(above(mid)), 63) <= t) most = mid;
+      if (__builtin_amdgcn_readlane(wave_scan(above(mid)), 63) <= t) most = mid;
       else k = mid + 1;
     }
     const int longer = above(k), like = above(k - 1) - longer;
-    const int rest = t - __builtin_amdgcn_readlane(lanes_scan(longer), 63);
-    const int end = lanes_scan(like);
+    const int rest = t - __builtin_amdgcn_readlane(wave_scan(longer), 63);
+    const int end = wave_scan(like);
     const uint64_t hit = __ballot(rest >= end - like && rest < end);
     if (!hit) return Place8{-1, 0, s};
     const int i = __ffsll((unsigned long long)hit) - 1;

@@ -227,4 +227,26 @@ __device__ __forceinline__ T wave_shfl_xor(T v, int mask) {
   return __shfl_xor(v, mask, 64);
 }
 
+// A wave's inclusive sums, by moves within rows of 16 lanes and of a row's last lane to those
+// behind it (numbers of 4 or 8 bytes; no LDS, whose latency six steps would have).
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T dpp_or_0(T v) {
+  constexpr int N = sizeof(T) / 4;
+  typedef int words __attribute__((ext_vector_type(N)));
+  words x = __builtin_bit_cast(words, v);
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_update_dpp(0, x[i], CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(T, x);
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += dpp_or_0<0x111, 0xF>(v);  // row_shr by 1, 2, 4, 8
+  v += dpp_or_0<0x112, 0xF>(v);
+  v += dpp_or_0<0x114, 0xF>(v);
+  v += dpp_or_0<0x118, 0xF>(v);
+  v += dpp_or_0<0x142, 0xA>(v);  // row_bcast of lane 15, then of lane 31
+  v += dpp_or_0<0x143, 0xC>(v);
+  return v;
+}
+
 }  // namespace pipo

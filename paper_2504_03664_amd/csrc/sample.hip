@@ -239,11 +239,7 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
   out.bin[tid] = h;
   // whole bins, as many as the list takes
   int c = (int)(h >> kCountShift);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(c, d, 64);
-    if (lane >= d) c += y;
-  }
+  c = wave_scan(c);
   if (lane == 63) scan[tid >> 6] = c;
   __syncthreads();
   for (int w = 0; w < tid >> 6; ++w) c += scan[w];
@@ -296,7 +292,8 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
 // small, since most of it runs once and is fetched as it runs.
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
 constexpr int kHeld = 1024;     // tokens of one bin that a wave keeps at hand
-constexpr u64 kNone = ~0ull;    // in place of a token (its logit a NaN)
+constexpr u64 kNone = ~0ull;    // in place of a token (its logit a NaN), behind all others
+constexpr int kShares = kRowThreads / kRank;
 static_assert(kRowThreads >= kBins, "a thread for each bin");
 
 // exp(-r / 8) 2^-kUnitBits, the weight of a unit of bin r over the first bin's middle, and
@@ -321,9 +318,8 @@ struct RowLds {
   u64 w[kBins], cum_c[kBins];        // a bin's units; counts up to each
   u64 bins_c[kBins];
   u64 sub_w[kBins], sub_c[kBins];    // of parts of a bin
-  u64 key[kRank], unit[kRank];
-  u64 part[kRowWaves];
-  double dpart[kRowWaves];
+  u64 key[kRank], unit[kRank], before[kShares][kRank];
+  u64 part[kRowWaves], part2[kRowWaves];
   u64 cand[kCands];                  // (key, index) of listed tokens, by bin
   u64 held[kRowWaves][kHeld];        // of one bin's, or of a piece of the row
   uint32_t info[kMaxSlices];         // a slice's bins below the row's, listed bins and tokens
@@ -355,20 +351,31 @@ __device__ __forceinline__ int place_for(RowLds& lds) {
   return __builtin_amdgcn_readfirstlane(at) + mine;
 }
 
-// inclusive sums over the first kBins threads' values
-template <typename T>
-__device__ __forceinline__ T scan_bins(T v, T (&part)[kRowWaves]) {
-  const int tid = threadIdx.x, lane = tid & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const T y = __shfl_up(v, d, 64);
-    if (lane >= d) v += y;
+// inclusive sums over the first kBins threads' values, two at a time
+template <typename A, typename B>
+__device__ __forceinline__ void scan_bins(A& v, B& w, RowLds& lds) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  A* const vs = reinterpret_cast<A*>(lds.part);
+  B* const ws = reinterpret_cast<B*>(lds.part2);
+  v = wave_scan(v);
+  w = wave_scan(w);
+  if ((tid & 63) == 63) {
+    vs[wave] = v;
+    ws[wave] = w;
   }
-  if (lane == 63) part[tid >> 6] = v;
   __syncthreads();
-  for (int w = 0; w < tid >> 6; ++w) v += part[w];
+  A a{};
+  B b{};
+#pragma unroll
+  for (int k = 0; k < kBins / 64 - 1; ++k) {
+    const A x = vs[k];
+    const B y = ws[k];
+    a += k < wave ? x : A{};
+    b += k < wave ? y : B{};
+  }
+  v += a;
+  w += b;
   __syncthreads();
-  return v;
 }
 
 // Where a place is looked for: at a rank (from 1) or where the units so far are above the
@@ -451,53 +458,48 @@ struct Row {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     u64* out = lds.held[wave];
     int n = 0;
-    const auto take = [&](float y, int i) {
-      const uint64_t hit = __ballot(__builtin_fabsf(y - mid) <= half);
-      if (hit) {
-        const int p = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(hit >> 32),
-                                                    __builtin_amdgcn_mbcnt_lo((uint32_t)hit, 0));
-        if ((hit >> lane & 1) && p < kHeld) out[p] = (uint32_t)i;
-        n += __popcll(hit);
-      }
+    // a bit for each of this lane's numbers, whose places follow those of the lanes before it
+    const auto near = [&](float y) { return __builtin_fabsf(y - mid) <= half; };
+    const auto note = [&](uint32_t marks, auto index) {
+      const int upto = wave_scan((int)__popc(marks));
+      for (int p = n + upto - __popc(marks); marks; ++p, marks &= marks - 1)
+        if (p < kHeld) out[p] = (uint32_t)index(__ffs(marks) - 1);
+      n += __builtin_amdgcn_readlane(upto, 63);
     };
-    // up to the first 16-byte boundary, from there by four, and the rest
+    // from the first 16-byte boundary by four, and up to three before and behind these
     const int head = min((int)(-(reinterpret_cast<uintptr_t>(x) >> 2) & 3), a.V);
-    int i0 = head;
-    f4 v[2][N];
-    const auto ask = [&](f4(&y)[N], int i) {
+    const int end = head + (a.V - head) / 4 * 4, i_edge = tid < head ? tid : end + tid - head;
+    const float edge = i_edge < a.V ? x[i_edge] : NAN;
+    if (head < end) {
+      f4 v[2][N];
+      const auto ask = [&](f4(&y)[N], int i) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) y[j] = *reinterpret_cast<const f4*>(x + i + 4 * (j * kRowThreads + tid));
-    };
-    const auto sift = [&](const f4(&y)[N], int i) {
+        for (int j = 0; j < N; ++j)
+          y[j] = *reinterpret_cast<const f4*>(x + min(i + 4 * (j * kRowThreads + tid), end - 4));
+      };
+      const auto sift = [&](const f4(&y)[N], int i0) {
+        uint32_t marks = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j) {
+          uint32_t four = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) take(y[j][e], i + 4 * (j * kRowThreads + tid) + e);
-    };
-    constexpr int kPiece = 4 * N * kRowThreads;
-    if (i0 + kPiece <= a.V) ask(v[0], i0);
+          for (int e = 0; e < 4; ++e) four |= near(y[j][e]) ? 1u << (4 * j + e) : 0;
+          marks |= i0 + 4 * (j * kRowThreads + tid) < end ? four : 0;
+        }
+        note(marks, [&](int bit) { return i0 + 4 * ((bit >> 2) * kRowThreads + tid) + (bit & 3); });
+      };
+      constexpr int kPiece = 4 * N * kRowThreads;
+      ask(v[0], head);
 #pragma unroll 1
-    while (i0 + kPiece <= a.V) {
-      if (i0 + 2 * kPiece <= a.V) ask(v[1], i0 + kPiece);
-      sift(v[0], i0);
-      i0 += kPiece;
-      if (i0 + kPiece > a.V) break;
-      if (i0 + 2 * kPiece <= a.V) ask(v[0], i0 + kPiece);
-      sift(v[1], i0);
-      i0 += kPiece;
-    }
-    constexpr int T = 16;
-    for (int i1 = i0 - head; i1 < a.V; i1 += T * kRowThreads) {
-      float v[T];
-#pragma unroll
-      for (int j = 0; j < T; ++j) v[j] = x[min(i1 + head + j * kRowThreads + tid, a.V - 1)];
-#pragma unroll
-      for (int j = 0; j < T; ++j) {
-        const int i = i1 + head + j * kRowThreads + tid;
-        take(i < a.V ? v[j] : NAN, i);
+      for (int i0 = head; i0 < end; i0 += 2 * kPiece) {
+        if (i0 + kPiece < end) ask(v[1], i0 + kPiece);
+        sift(v[0], i0);
+        if (i0 + kPiece >= end) break;
+        if (i0 + 2 * kPiece < end) ask(v[0], i0 + 2 * kPiece);
+        sift(v[1], i0 + kPiece);
       }
     }
-    if (wave == 0) take(tid < head ? x[min(tid, a.V - 1)] : NAN, tid);
+    note(wave == 0 && near(edge), [&](int) { return i_edge; });
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (other lanes' entries)
     __builtin_amdgcn_wave_barrier();
     const bool over = n > kHeld;
@@ -550,7 +552,10 @@ struct Row {
     const int tid = threadIdx.x;
     __syncthreads();
     const u64 c = tid < kBins ? lds.sub_c[tid] : 0, w = tid < kBins ? lds.sub_w[tid] : 0;
-    const u64 cc = c0 + scan_bins(c, lds.part), cw = w0 + scan_bins(w, lds.part);
+    u64 cc = c, cw = w;
+    scan_bins(cc, cw, lds);
+    cc += c0;
+    cw += w0;
     const int part = first_of(c > 0 && q.passes(cc, cw), kBins - 1, lds);
     if (tid == part) {
       lds.part[0] = cc - c;
@@ -646,8 +651,9 @@ struct Row {
       hi = min(hi, lo + ((1u << shift) - 1));
     }
     if (n > kRank) return pick_equal(lo, n, c0, w0, q);
-    // in order: every token finds its place among the others
+    // in order: every token finds its place among the others, a share of them a thread
     if (tid == 0) lds.n = 0;
+    if (tid < kRank) lds.key[tid] = kNone;
     __syncthreads();
     each([&](uint32_t d, int i, int b, uint32_t f) {
       if (!mine(d, b, f)) return;
@@ -658,16 +664,28 @@ struct Row {
     });
     __syncthreads();
     n = min(lds.n, kRank);
-    u64 key = 0, c = c0, w = w0;
-    if (tid < n) {
-      key = lds.key[tid];
-#pragma unroll 4
-      for (int j = 0; j < n; ++j) {
-        const bool before = lds.key[j] <= key;
-        c += before;
-        w += before ? lds.unit[j] : 0;
-      }
+    const u64 key = lds.key[tid % kRank];
+    constexpr int N = kRank / kShares;   // of a share, which a wave has in its lanes
+    static_assert(N <= 64 && kRank % 64 == 0, "a wave's threads have one share");
+    const int share = __builtin_amdgcn_readfirstlane(tid / kRank), shares = n <= N ? 1 : kShares;
+    const int theirs = min((int)n - N * share, N);
+    const u64 other = lds.key[N * share + (tid & (N - 1))], unit = lds.unit[N * share + (tid & (N - 1))];
+    const auto of = [](u64 x, int i) {
+      return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), i) << 32 |
+             (uint32_t)__builtin_amdgcn_readlane((int)x, i);
+    };
+    u64 c = 0;
+#pragma unroll 2
+    for (int j = 0; j < theirs; ++j) c += of(other, j) <= key ? of(unit, j) + (1ull << kCountShift) : 0;
+    if (shares > 1) {
+      lds.before[share][tid % kRank] = c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int k = 0; k < kShares; ++k) c += lds.before[k][tid % kRank];
     }
+    const u64 w = w0 + (c & ((1ull << kCountShift) - 1));
+    c = c0 + (c >> kCountShift);
     // of those that pass the one with the fewest before it, or the last of all
     int rank = tid < n && q.passes(c, w) ? (int)(c - c0) : (int)n;
 #pragma unroll
@@ -719,11 +737,7 @@ struct Row {
         if (i < a.V) marks |= (uint32_t)(x[i] == v) << j;
       }
       int run = __popc(marks);
-#pragma unroll
-      for (int k = 1; k < 64; k *= 2) {
-        const int z = __shfl_up(run, k, 64);
-        if (lane >= k) run += z;
-      }
+      run = wave_scan(run);
       if (lane == 63) lds.redi[tid >> 6] = run;
       __syncthreads();
       int total = 0;
@@ -864,8 +878,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_rows_k(SampleArgs a) {
     }
   }
   // (over the first bin's middle: equal logits there are summed and divided exactly)
-  const double cum_w = scan_bins((double)w * factor, lds.dpart);
-  const u64 cum_c = scan_bins(c, lds.part);
+  double cum_w = (double)w * factor;
+  u64 cum_c = c;
+  scan_bins(cum_w, cum_c, lds);
   if (tid < kBins) {
     lds.factor[tid] = factor;
     lds.per[tid] = per;

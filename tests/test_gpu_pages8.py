@@ -201,7 +201,7 @@ def check(got, want, tol, what):
 
 def check_error(got, want, many, what=""):
     """all in all: the output's rounding (rms 2^-11 / root 3), and one of the weights"""
-    if want.size > 500:
+    if want.size > 500 and want.any():   # (zeros, of rows that see nothing, are equal)
         err = np.linalg.norm(got.astype(np.float64) - want) / np.linalg.norm(want)
         assert err <= np.sqrt((2 if many else 1) / 3) * HALF * 1.1, (what, err)
 

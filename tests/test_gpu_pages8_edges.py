@@ -1,0 +1,215 @@
+"""The 8-bit pages' attention and the draw of tokens where their work is shared out in another way:
+long contexts whose pages a wave looks up more than once, launches of short and long workgroups,
+rows shared out anew between replays, streams side by side, bins of a row at the sizes where
+their tokens are found otherwise.  Tolerances as in test_gpu_pages8.py and test_gpu_sample.py."""
+import numpy as np
+import pytest
+
+from oracle import pages8 as O
+from paper_2504_03664_amd import binding as B
+from paper_2504_03664_amd.binding import DeviceBuffer as DB
+from test_gpu_pages import Hip
+from test_gpu_pages8 import BOTH, HALF, Cache, attend, check, dev, draw_q, run_attention, want_attention
+from test_gpu_sample import check as check_draw
+
+pytestmark = pytest.mark.gpu
+
+
+def with_holes(c, q, rows, H, table):
+    """(values, tolerance) of plain attention, keys on entries that are no pages left out"""
+    out, tol, at = [], [], 0
+    many = max(rows) * (H // c.Hkv) > 64
+    for i, (r, n) in enumerate(zip(rows, c.lens)):
+        gone = np.repeat((table[i] < 0) | (table[i] >= c.n_pages), c.ps)[:n]
+        x = q[at:at + r].reshape(r, H, c.D).astype(np.float64)
+        k, v = c.k[i].values(), c.v[i].values()
+        seen, y, most = O.seen(r, n) & ~gone, np.zeros(x.shape), 0.0
+        for h in range(H):
+            kh = h // (H // c.Hkv)
+            s = np.where(seen, x[:, h] @ k[:, kh].T, -np.inf)
+            most = max(most, (np.abs(x[:, h]) @ np.abs(k[:, kh]).T).max())
+            p = np.exp(s - np.maximum(s.max(1, keepdims=True), -1e300))
+            total = p.sum(1, keepdims=True)
+            y[:, h] = p @ v[:, kh] / np.where(total > 0, total, 1)
+        step = (c.D * 2.0 ** -24 + 2.0 ** -22) * most
+        out.append(y.reshape(r, -1))
+        tol.append(HALF * np.abs(out[-1]) + (2 * step + (HALF if many else 2.0 ** -20)) * np.abs(v).max() +
+                   2.0 ** -25)
+        at += r
+    return np.concatenate(out), np.concatenate(tol)
+
+
+@BOTH
+@pytest.mark.parametrize("n,rows", [(9000, [1]), (9000, [70]), (17000, [1, 2])])
+def test_holes_over_a_long_context(n, rows, fmt):
+    """Each wave's blocks go past the 32 or 64 that it looks up at a time."""
+    print(f"holes n={n} rows={rows} {fmt}", flush=True)
+    rng = np.random.default_rng(n + len(rows))
+    c = Cache([n - 1000 * i for i in range(len(rows))], 1, 64, 16, fmt, rng)
+    c.fill(rng)
+    t = c.table.copy()
+    bad = rng.random(t.shape) < 0.2
+    t[bad] = rng.choice([-1, c.n_pages, 1 << 30, -(1 << 31)], int(bad.sum()))
+    c.set_table(t)
+    q = draw_q(rng, sum(rows), 2, 64)
+    want, tol = with_holes(c, q, rows, 2, t)
+    for split in (True, False):
+        check(attend(c, q, rows, 2, split=split)[:len(q)], want, tol, f"split={split}")
+
+
+@BOTH
+@pytest.mark.parametrize("n,lo,hi", [(40, 100, 260), (70, 1, 200)])
+def test_many_tiles(n, lo, hi, fmt):
+    """More tiles of columns than compute units, of prompts with and without a context, with all
+    that scores can have, and plain."""
+    print(f"tiles n={n} {fmt}", flush=True)
+    rng = np.random.default_rng(n)
+    rows = [int(x) for x in rng.integers(lo, hi, n)]
+    lens = [max(0, r + int(x)) for r, x in zip(rows, rng.choice([-30, 0, 0, 17, 300], n))]
+    run_attention(lens, rows, 4, 4, 128, 32, fmt)
+    run_attention(lens, rows, 4, 4, 128, 32, fmt, cap=8.0, slopes=True, window=90, prefix=40, seed=2)
+
+
+@pytest.mark.parametrize("lens", [[64, 64, 64], [1, 1, 1], [0, 0, 0], [5000, 64, 0], [129, 128, 127]])
+def test_tiles_of_like_and_unlike_sequences(lens):
+    """Prompts with as many keys as others, with none, and with more rows than keys."""
+    print(f"tiles lens={lens}", flush=True)
+    for rows in ([300, 300, 300], [400, 65, 0], [129, 1, 257]):
+        run_attention(lens, rows, 3, 1, 64, 16, "int8")
+
+
+def test_rows_shared_out_anew():
+    """A captured call whose rows are shared out in another way at every replay: prompts,
+    single rows, none, rows behind the last sequence."""
+    hip, rng = Hip(), np.random.default_rng(21)
+    lens, H, Hkv, D, M = [700, 90, 1500, 130], 8, 2, 64, 140
+    c = Cache(lens, Hkv, D, 32, "e4m3", rng)
+    c.fill(rng)
+    q = draw_q(rng, M, H, D)
+    dq, do, do2, start, dl = dev(q), DB(M * H * D * 2), DB(M * H * D * 2), DB(4 * 5), dev(lens, np.int32)
+    f = B.PipoAttnScores(9.0, 0, None, None, 0)
+    n = B.pipo_op_attn_kv8_pages_workspace_bytes(c.c(), f, H, M, 130, 1500)
+    assert n > 0
+    ws, ws2, stream = DB(n), DB(n), hip.stream()
+
+    def run(o, ws, st):
+        B.pipo_op_attn_kv8_pages(c.c(), 0, f, dq.ptr, H * D, start.ptr, dl.ptr, o.ptr, H * D, H, M, 130,
+                                 1500, ws.ptr, n, st)
+
+    def put(buf, a):
+        a = np.ascontiguousarray(a)
+        assert B.lib().pipo_copy_h2d(buf.ptr, a.ctypes.data, a.nbytes) == 0
+
+    put(start, np.arange(5, dtype=np.int32))
+    graph = hip.capture(stream, lambda: run(do2, ws2, stream))
+    for rows in ([1, 1, 1, 1], [130, 1, 1, 1], [0, 90, 9, 40], [1, 2, 130, 7], [0, 0, 0, 0], [17, 16, 15, 92]):
+        put(start, np.concatenate([[0], np.cumsum(rows)]).astype(np.int32))
+        for o in (do, do2):
+            put(o, np.full(M * H * D, 9, np.float16))
+        run(do, ws, None)
+        B.pipo_dev_synchronize()
+        hip("hipGraphLaunch", graph, stream)
+        hip("hipStreamSynchronize", stream)
+        got = [o.to_array(np.float16, (M, H * D)) for o in (do, do2)]
+        assert np.array_equal(got[0].view(np.uint16), got[1].view(np.uint16))
+        m = sum(rows)
+        assert (got[0][m:] == 9).all()
+        if m:
+            want, tol = want_attention(c, q[:m], rows, lens, H, cap=9.0)
+            # (130 rows are planned for: any weights may be rounded)
+            check(got[0][:m], want, tol, rows)
+
+
+def test_two_streams_at_once():
+    """Two sequences of calls side by side, each with a workspace of its own, give what
+    they give one after the other."""
+    hip, rng = Hip(), np.random.default_rng(22)
+    H, Hkv, D, V, n = 8, 2, 128, 60000, 12
+    streams, jobs = [hip.stream(), hip.stream()], []
+    for fmt, most in (("e4m3", 1), ("int8", 40)):
+        lens, rows = [int(x) for x in rng.integers(1000, 3000, n)], [most] * n
+        c = Cache(lens, Hkv, D, 64, fmt, rng)
+        c.fill(rng)
+        f = B.PipoAttnScores(20.0, 0, None, None, 0)
+        M = sum(rows)
+        a_n = B.pipo_op_attn_kv8_pages_workspace_bytes(c.c(), f, H, M, most, max(lens))
+        s_n = B.pipo_op_sample_workspace_bytes(n, V)
+        d = dict(q=dev(draw_q(rng, M, H, D)), o=DB(M * H * D * 2), ws=DB(max(a_n, s_n, 16)),
+                 start=dev(np.concatenate([[0], np.cumsum(rows)]), np.int32), lens=dev(lens, np.int32),
+                 x=dev(rng.standard_normal((n, V)) * 2, np.float32), u=dev(rng.random(n), np.float32),
+                 p=dev(rng.choice([1.0, 0.9], n), np.float32), next=DB(4 * n), logp=DB(4 * n))
+
+        def job(st, c=c, f=f, d=d, M=M, most=most, top=max(lens), a_n=a_n, s_n=s_n):
+            B.pipo_op_attn_kv8_pages(c.c(), 0, f, d["q"].ptr, H * D, d["start"].ptr, d["lens"].ptr,
+                                     d["o"].ptr, H * D, H, M, most, top, d["ws"].ptr, a_n, st)
+            B.pipo_op_sample(d["x"].ptr, V, None, None, d["p"].ptr, None, d["u"].ptr, d["next"].ptr,
+                             d["logp"].ptr, n, V, d["ws"].ptr, s_n, st)
+
+        jobs.append((job, d, M))
+
+    def results():
+        return [(d["o"].to_array(np.uint16, (M, H * D)), d["next"].to_array(np.int32, (n,)),
+                 d["logp"].to_array(np.uint32, (n,))) for _, d, M in jobs]
+
+    for job, _, _ in jobs:
+        job(None)
+    B.pipo_dev_synchronize()
+    first = results()
+    for _ in range(3):
+        for _ in range(4):
+            for (job, _, _), st in zip(jobs, streams):
+                job(st)
+        for st in streams:
+            hip("hipStreamSynchronize", st)
+        for a, b in zip(first, results()):
+            assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("V", [20000, 20001, 20002, 20003, 33000])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+def test_far_tokens_anywhere(V, shift):
+    """Tokens that no slice lists, drawn at a row's ends, at steps of 16384 and between:
+    each is asked for by the middle of its own share."""
+    rng = np.random.default_rng(V + shift)
+    at = sorted({0, 1, 2, 3, 4, 16379 % V, 16380, 16383, 16384, 16385, V // 2, *range(V - 6, V)})
+    x = (rng.standard_normal((len(at), V)) * 2).astype(np.float32)
+    x[:, at] = (1 + rng.random((len(at), len(at))) * 0.5).astype(np.float32)
+    u = []
+    for row, i in zip(x.astype(np.float64), at):
+        order = np.lexsort((np.arange(V), -row))
+        w = np.exp(row[order] - row.max())
+        before = np.concatenate([[0], np.cumsum(w)])
+        j = int(np.flatnonzero(order == i)[0])
+        u.append((before[j] + before[j + 1]) / 2 / before[-1])
+    got, _ = check_draw(x, np.array(u), pad=1, shift=shift)
+    assert list(got) == at
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 64, 65, 96, 127, 128, 129, 257, 1100])
+def test_bins_of_every_size(n, workspace):
+    """n different logits, or n of which many are equal, within an eighth, under one larger."""
+    rng = np.random.default_rng(n)
+    rows, V = 8, 9001
+    for values in (1 + rng.random((rows, n)) * 0.124, 1 + rng.integers(0, 4, (rows, n)) * 0.03):
+        x = np.full((rows, V), -6.0, np.float32)
+        for i in range(rows):
+            where = rng.permutation(V)[:n + 1]
+            x[i, where[:n]], x[i, where[n]] = values[i], 2.0
+        u = np.concatenate([[0.0, 0.999], rng.random(rows - 2)])
+        check_draw(x, u, workspace=workspace)
+        check_draw(x, u, k=rng.integers(1, n + 2, rows), p=rng.random(rows), workspace=workspace)
+        check_draw(x, u, m=np.exp(-1 + rng.random(rows) * 0.13), workspace=workspace)
+
+
+def test_logits_far_from_zero_and_apart():
+    """Bins found from sums whose exponents differ: logits of any size beside the largest."""
+    rng = np.random.default_rng(23)
+    rows, V = 12, 9000
+    for base, T in ((0.0, 1.0), (3e4, 1.0), (-3e4, 0.5), (1e6, 30.0), (-2.5e5, 8.0), (1e-30, 1.0)):
+        x = (base + rng.standard_normal((rows, V)) * T).astype(np.float32)
+        for i, far in enumerate((-1e38, -3e38, -np.inf, -1e5, -2.0 ** 17, -2.0 ** 18, -2.0 ** 19,
+                                 -2.0 ** 20, -2.0 ** 21, -1e9, -65.0, -33.0)):
+            x[i, rng.integers(0, V, 400)] = min(far, base - abs(far) * 1e-3) if far != -np.inf else far
+        check_draw(x, rng.random(rows), T=np.full(rows, T))

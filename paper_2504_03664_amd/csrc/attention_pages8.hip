@@ -137,6 +137,13 @@ __device__ __forceinline__ void put(const Attn8& a, int h, int row, int sp, int 
 // that take the split's blocks of 32 keys by turns, straight into registers in operand
 // order, the next block's loads under way while one is worked on.  Weights go to
 // the second product as a high and a low half, 22 bits.
+//
+// Many sequences are bound by HBM: 64 of 2048 keys, 8 heads of 128, 45 us, 6.0 TB/s; 64 of 544
+// keys, 56 heads, 79 us, 6.3 TB/s.  Few are bound by trips to memory that wait for each
+// other, lengths (1.2 us), scales and tiles (3 us to the end of a wave's first block, 1.2 us
+// for each of the next), and by the join (1 us in the workgroup, 3 in the kernel that adds
+// splits): 16 of 100 to 2100 keys 17.7 us where 7.6 us of bytes are.  Loads three blocks ahead
+// and more splits gave nothing.
 template <int D>
 struct Block8 {
   u32x4 k[2][D / 64], v[2][D / 64];
@@ -357,6 +364,14 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 // all of them work on this one, so a block is unpacked once for 128 columns and every LDS
 // access is a wave's contiguous kilobyte.  Weights are rounded to a half, and it is the
 // rounded ones that are added up to divide by.
+//
+// 8 sequences of 509 rows over 4099 keys, 32 heads over 8 of 128: 281 to 288 us, 890 to 914
+// TFLOP/s (a 8192^3 product of the library: 1139).  Vector instructions (softmax, codes to
+// halves) take 41 % of a SIMD's cycles and matrix ones 27 %, and a wave has little to put
+// beside its own softmax but the last block's second product.  A workgroup's start (place,
+// first keys) takes 5 us and its end 2, so short prompts reach less: 8 of 512 rows 43 us,
+// 400 TFLOP/s; cap, bias and prefix together 51 us.  Teams with the workgroup's
+// barriers in turn, one of matrix and one of vector work, were slower than barriers of their own.
 
 // The t-th column tile of the launch: its sequence (-1: none) and which of the
 // sequence's tiles.  Only sequences of many columns have tiles.  The tiles of up to 64
@@ -811,7 +826,9 @@ __device__ __forceinline__ int seq_of_row(const Attn8& a, int m) {
 
 // Adds the splits of a row's head, in order: WAVES waves take them by turns, each asking for
 // EACH at once, D / 64 dimensions a lane, and are added in order.  What there may be is
-// asked for before the row's sequence is known.
+// asked for before the row's sequence is known.  Bound by two trips to memory (2.8 us a launch
+// for 16 rows of 32 heads and 2 splits, 3.8 us for one row of 32 splits, where a wave that
+// reads them in turn takes 6).
 template <int D, int WAVES, int EACH>
 __global__ __launch_bounds__(256) void attn8_merge_k(Attn8 a) {
   constexpr int N = D / 64, HEADS = 4 / WAVES;
@@ -875,6 +892,17 @@ static int chunk_of(int64_t keys, int64_t S, int block) {
   return (int)std::max<int64_t>(block, ((keys + S - 1) / S + block - 1) / block * block);
 }
 
+// Splits and shares, by sizes alone, measured on both sides (us, 8 heads of 128, 4 query heads
+// each unless said):
+//   waves: 8 where workgroups are up to one a CU (16 sequences 17.9, by 4 waves 20.8), else
+//          4, two workgroups a CU and no more (64 of 56 heads 82, by 8 waves 111; 64 of 8
+//          heads 44.8 and 46.4; 128 of them 90 and 88);
+//   chunk_few: from kSplitFew keys up to as many splits as fill the CUs, of kMinFew keys at
+//          least (one sequence of 65000 27.8, unsplit 330; one of 2000 11.5 and 15.8; 500
+//          keys are not split, 8.3);
+//   chunk_many: the same with a few columns' tiles, of kMinMany keys at least;
+//   teams: 2 where tiles are at most one a CU, or two with long contexts (4 of 509 rows over
+//          up to 4099 keys 97, by one team 126), else 1 (8 of 512 rows 43, by two 62).
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
 struct Plan8 {
   bool few, many;   // sequences that may be of either kind
@@ -958,7 +986,7 @@ static void launch_attn8(const Attn8& a, const Plan8& p, hipStream_t st) {
     else
       launch(attn8_many_k<D, INT8, MOD, 1>, g, dim3(256), 0, st, a);
   }
-  constexpr int kSmallMerge = 8;
+  constexpr int kSmallMerge = 8;   // (up to here a wave has all of a head's splits under way)
   if (p.splits() > kSmallMerge)
     launch(attn8_merge_k<D, 4, kMaxSplits / 4>, dim3((unsigned)a.M, (unsigned)a.H), dim3(256), 0, st, a);
   else if (p.splits() > 1)

@@ -367,7 +367,7 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 //
 // 8 sequences of 509 rows over 4099 keys, 32 heads over 8 of 128: 281 to 288 us, 890 to 914
 // TFLOP/s (a 8192^3 product of the library: 1139).  Vector instructions (softmax, codes to
-// halves) take 41 % of a SIMD's cycles and matrix ones 27 %, and a wave has little to put
+// halves) take 47 % of a SIMD's cycles and matrix ones 31 %, and a wave has little to put
 // beside its own softmax but the last block's second product.  A workgroup's start (place,
 // first keys) takes 5 us and its end 2, so short prompts reach less: 8 of 512 rows 43 us,
 // 400 TFLOP/s; cap, bias and prefix together 51 us.  Teams with the workgroup's

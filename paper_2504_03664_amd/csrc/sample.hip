@@ -175,7 +175,7 @@ __device__ __forceinline__ int block_min(int v, int (&lds)[W]) {
 // its bins, so nothing of other slices is waited for; every logit costs one LDS atomic,
 // by bin, on a word that holds the bin's units and count, and 28 vector instructions, of
 // which 17 make a weight: they are what bounds 128 rows of 128256 (21 us, 3.1 TB/s; the vector
-// units are busy for two thirds of it, LDS for a quarter).
+// units are busy for two thirds of it, LDS for 30 %).
 template <int E>
 __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
   static_assert(E <= 32 && 256 * E <= kSliceMax, "a bin's count and weight fit a word");

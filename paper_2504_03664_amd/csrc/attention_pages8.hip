@@ -192,19 +192,22 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 
   // lane 2 i + j holds the page and the scales of tile j of the wave's i-th block, 32
   // blocks at a time
-  int turn = 32;
-  bool known = a.window <= 0;
+  int turn = 0;
   float2 scales = make_float2(1.f, 1.f);
+  const auto look_up = [&](int b, bool known) {
+    const int64_t mb = (int64_t)b + (lane >> 1) * W;
+    const int pos = mb < b1 ? key_of((int)mb) + 16 * (lane & 1) : INT32_MAX;
+    if (!known) pages = pos < s.len ? table[pos >> a.c.ps_log2] : -1;
+    if (pos >= s.len || pages < 0 || pages >= a.c.n_pages) pages = -1;
+    scales = make_float2(1.f, 1.f);
+    if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
+    turn = 0;
+  };
   const auto load = [&](Block8<D>& x, int b) {
     if (turn == 32) {
-      turn = 0;
-      const int64_t mb = (int64_t)b + (lane >> 1) * W;
-      const int pos = mb < b1 ? key_of((int)mb) + 16 * (lane & 1) : INT32_MAX;
-      if (!known) pages = pos < s.len ? table[pos >> a.c.ps_log2] : -1;
-      if (pos >= s.len || pages < 0 || pages >= a.c.n_pages) pages = -1;
-      scales = make_float2(1.f, 1.f);
-      if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
-      known = false;
+      look_up(b, false);
+      // (waited for here, lest every block waits for its last loads where these may be on their way)
+      asm volatile("" : "+v"(pages), "+v"(scales.x), "+v"(scales.y));
     }
     const int key = key_of(b);
 #pragma unroll
@@ -317,16 +320,26 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
     }
   };
 
-  Block8<D> x0, x1;
-  if (b < b1) load(x0, b);
-  while (b < b1) {
-    if (b + W < b1) load(x1, b + W);
+  // The next block's loads stay under way only where no path leaves it open which are, so
+  // the last blocks are apart, and all of it is in one branch.
+  if (b < b1) {
+    Block8<D> x0, x1;
+    look_up(b, a.window <= 0);
+    load(x0, b);
+    for (; b + 2 * W < b1; b += 2 * W) {
+      load(x1, b + W);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(x0, b);
+      __builtin_amdgcn_sched_barrier(0);
+      load(x0, b + 2 * W);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(x1, b + W);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const bool two = b + W < b1;
+    if (two) load(x1, b + W);
     compute(x0, b);
-    b += W;
-    if (b >= b1) break;
-    if (b + W < b1) load(x0, b + W);
-    compute(x1, b);
-    b += W;
+    if (two) compute(x1, b + W);
   }
 
   // join the waves: element e of acc[n] is dimension 16 n + 4 g + e of column r
@@ -521,8 +534,8 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   const int32_t* table = a.c.table + si * a.c.stride;
   int pages = -1;
   float2 scales = make_float2(1.f, 1.f);
-  const auto fetch_k = [&](int blk) {
-    if ((blk & 63) == 0) {
+  const auto fetch_k = [&](int blk, bool first) {
+    if (first || (blk & 63) == 0) {
       pages = -1;
       scales = make_float2(1.f, 1.f);
       if (blk + lane < mine) {
@@ -531,6 +544,8 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
         if (pages < 0 || pages >= a.c.n_pages) pages = -1;
         if (pages >= 0) scales = *reinterpret_cast<const float2*>(scales8_at(a.c, pages, kh, pos));
       }
+      // (waited for here, lest every block waits for its last loads where these may be on their way)
+      if (!first) asm volatile("" : "+v"(pages), "+v"(scales.x), "+v"(scales.y));
     }
     const int page = __builtin_amdgcn_readlane(pages, blk & 63);
     ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scales.x), blk & 63));
@@ -568,7 +583,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
     }
   };
 
-  if (mine > 0) fetch_k(0);
+  if (mine > 0) fetch_k(0, true);
   h8 qf[U][KK];
   float slope[U];
 #pragma unroll
@@ -721,7 +736,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
   if (mine > 0) {
     unpack_k(0);
     fetch_v(0);
-    if (mine > 1) fetch_k(1);
+    if (mine > 1) fetch_k(1, false);
   }
   __syncthreads();
 #pragma unroll 1
@@ -730,7 +745,7 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
     if (i + 1 < mine) {
       unpack_k(i + 1);
       fetch_v(i + 1);
-      if (i + 2 < mine) fetch_k(i + 2);
+      if (i + 2 < mine) fetch_k(i + 2, false);
     }
     if (!idle) {
       if (i > 0) add_block(i - 1);

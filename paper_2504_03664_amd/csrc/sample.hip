@@ -498,13 +498,13 @@ struct Row {
         note(marks, [&](int bit) { return i0 + 4 * ((bit >> 2) * kRowThreads + tid) + (bit & 3); });
       };
       constexpr int kPiece = 4 * N * kRowThreads;
+      // (asked for on every path, also past the end, else each piece would wait for the next)
       ask(v[0], head);
 #pragma unroll 1
       for (int i0 = head; i0 < end; i0 += 2 * kPiece) {
-        if (i0 + kPiece < end) ask(v[1], i0 + kPiece);
+        ask(v[1], i0 + kPiece);
         sift(v[0], i0);
-        if (i0 + kPiece >= end) break;
-        if (i0 + 2 * kPiece < end) ask(v[0], i0 + 2 * kPiece);
+        ask(v[0], i0 + 2 * kPiece);
         sift(v[1], i0 + kPiece);
       }
     }

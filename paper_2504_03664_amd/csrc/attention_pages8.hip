@@ -277,9 +277,10 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
         const int first = key0 + 16 * j + 4 * g;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
+          // (without branches)
           const int key = first + e;
-          const bool in = x.ok[j] && ((key >= mine.lo && key < mine.hi) || key < pre);
-          y[j][e] = in ? y[j][e] : -INFINITY;
+          const bool in = ((uint32_t)(key - mine.lo) < (uint32_t)(mine.hi - mine.lo)) | (key < pre);
+          y[j][e] = x.ok[j] & in ? y[j][e] : -INFINITY;
         }
         // codes of keys that do not exist may be anything
         const int n = x.ok[j] ? min(max(s.len - first, 0), 4) : 0;
@@ -691,16 +692,16 @@ __global__ __launch_bounds__(TEAMS * 256) __attribute__((amdgpu_waves_per_eu(2))
         const int col = c0 + 16 * u + r, qj = query_of(a, col), at = s.len - s.nq + qj;
         Seen see = Seen{0, 0};
         if (col < cols) see = seen_by(a, s, qj);
-        const int hi = see.hi - base, lo = see.lo - base, pre = (col < cols ? s.pre : 0) - base;
+        const int lo = see.lo - base, n = see.hi - see.lo, pre = (col < cols ? s.pre : 0) - base;
 #pragma unroll
         for (int j = 0; j < T; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int key = 16 * j + e;
-            const bool in = (valid >> j & 1) && ((key >= lo && key < hi) || key < pre);
+            const bool in = ((uint32_t)(key - lo) < (uint32_t)n) | (key < pre);   // (without branches)
             if constexpr (MOD)   // (keys past it: of a prefix)
               y[u][j][e] = __builtin_fmaf(slope[u], -2.f * (float)max(key - (at - base), 0), y[u][j][e]);
-            y[u][j][e] = in ? y[u][j][e] : -INFINITY;
+            y[u][j][e] = (bool)(valid >> j & 1) & in ? y[u][j][e] : -INFINITY;
           }
       }
     }

@@ -453,7 +453,8 @@ typedef struct {
  * pipo_op_attn_pages over these pages, with `scores` (read on the host during the call;
  * may be NULL).  Everything said there holds: rows and lengths, bounds, what is left as
  * it was, the workspace (of pipo_op_attn_kv8_pages_workspace_bytes bytes) and the limits.
- * A row that sees no key becomes 0.  Keys and values are read exactly, softmax and
+ * Of the table, a sequence's entries up to position max_len may be read.  A row that sees
+ * no key becomes 0.  Keys and values are read exactly, softmax and
  * sums in fp32, the output rounded once to fp16; where a sequence may have more than
  * 64 rows times query heads of a key/value head, weights are rounded to fp16 as well.
  */

@@ -138,12 +138,11 @@ __device__ __forceinline__ void put(const Attn8& a, int h, int row, int sp, int 
 // order, the next block's loads under way while one is worked on.  Weights go to
 // the second product as a high and a low half, 22 bits.
 //
-// Many sequences are bound by HBM: 64 of 2048 keys, 8 heads of 128, 45 us, 6.0 TB/s; 64 of 544
-// keys, 56 heads, 79 us, 6.3 TB/s.  Few are bound by trips to memory that wait for each
-// other, lengths (1.2 us), scales and tiles (3 us to the end of a wave's first block, 1.2 us
-// for each of the next), and by the join (1 us in the workgroup, 3 in the kernel that adds
-// splits): 16 of 100 to 2100 keys 17.7 us where 7.6 us of bytes are.  Loads three blocks ahead
-// and more splits gave nothing.
+// Many sequences are bound by HBM: 128 of 2048 keys, 8 heads of 128, 86 us, 6.2 TB/s; 64 of 544
+// keys, 56 heads, 78 us, 6.4 TB/s.  Few are bound by trips to memory that wait for each
+// other, lengths (1.2 us), scales and tiles (3 us to the end of a wave's first block), and
+// by the join (1 us in the workgroup, 3 in the kernel that adds splits): 16 of 100 to 2100
+// keys 17.5 us where 7.6 us of bytes are.
 template <int D>
 struct Block8 {
   u32x4 k[2][D / 64], v[2][D / 64];
@@ -379,19 +378,19 @@ __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2))) voi
 // access is a wave's contiguous kilobyte.  Weights are rounded to a half, and it is the
 // rounded ones that are added up to divide by.
 //
-// 8 sequences of 509 rows over 4099 keys, 32 heads over 8 of 128: 281 to 288 us, 890 to 914
+// 8 sequences of 509 rows over 4099 keys, 32 heads over 8 of 128: 278 to 282 us, 910 to 921
 // TFLOP/s (a 8192^3 product of the library: 1139).  Vector instructions (softmax, codes to
-// halves) take 47 % of a SIMD's cycles and matrix ones 31 %, and a wave has little to put
+// halves) take 48 % of a SIMD's cycles and matrix ones 32 %, and a wave has little to put
 // beside its own softmax but the last block's second product.  A workgroup's start (place,
-// first keys) takes 5 us and its end 2, so short prompts reach less: 8 of 512 rows 43 us,
-// 400 TFLOP/s; cap, bias and prefix together 51 us.  Teams with the workgroup's
+// first keys) takes 5 us and its end 2, so short prompts reach less: 8 of 512 rows 41 us,
+// 418 TFLOP/s; cap, bias and prefix together 51 us.  Teams with the workgroup's
 // barriers in turn, one of matrix and one of vector work, were slower than barriers of their own.
 
 // The t-th column tile of the launch: its sequence (-1: none) and which of the
 // sequence's tiles.  Only sequences of many columns have tiles.  The tiles of up to 64
 // sequences go by the keys that they may see, the most first: those that start when the
-// last ones end are short (8 prompts of 512 rows, 16 tiles each of 1 to 8 blocks: 66 us
-// sequence by sequence, 55 us so).
+// last ones end are short (8 prompts of 512 rows, 16 tiles each of 1 to 8 blocks, cap,
+// bias and prefix: 67 us sequence by sequence, 54.5 us so).
 struct Place8 {
   int seq, tile;
   Seq8 s;
@@ -910,15 +909,15 @@ static int chunk_of(int64_t keys, int64_t S, int block) {
 
 // Splits and shares, by sizes alone, measured on both sides (us, 8 heads of 128, 4 query heads
 // each unless said):
-//   waves: 8 where workgroups are up to one a CU (16 sequences 17.9, by 4 waves 20.8), else
-//          4, two workgroups a CU and no more (64 of 56 heads 82, by 8 waves 111; 64 of 8
-//          heads 44.8 and 46.4; 128 of them 90 and 88);
+//   waves: 8 where workgroups are up to one a CU (16 sequences 17.5, by 4 waves 18.7; but 32
+//          in a window 16.6 and 15.5), else 4, two workgroups a CU and no more (64 of 56
+//          heads 79, by 8 waves 107 to 111; 64 of 8 heads 45 and 47);
 //   chunk_few: from kSplitFew keys up to as many splits as fill the CUs, of kMinFew keys at
-//          least (one sequence of 65000 27.8, unsplit 330; one of 2000 11.5 and 15.8; 500
-//          keys are not split, 8.3);
+//          least (one sequence of 65000 27.6, unsplit 301; one of 2000 11.4 and 14.5, by
+//          twice the keys 12.5; 500 keys are not split, 8.4);
 //   chunk_many: the same with a few columns' tiles, of kMinMany keys at least;
 //   teams: 2 where tiles are at most one a CU, or two with long contexts (4 of 509 rows over
-//          up to 4099 keys 97, by one team 126), else 1 (8 of 512 rows 43, by two 62).
+//          up to 4099 keys 96, by one team 118), else 1 (8 of 512 rows 41, by two 61).
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
 struct Plan8 {
   bool few, many;   // sequences that may be of either kind

@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256) void sample_slices_k(SampleArgs a) {
 // share a SIMD.  The code is kept small, since most of it runs once and is fetched as it runs
 // (198 KB of it took 53 us for one row, 25 KB 25).  Bound by latencies: 5 us until
 // bins and lists are joined, 1.3 to 2.5 us for each of top-k, min-p, top-p and the draw
-// where the bin is listed; 9 us to look for a bin that is not (128256 logits, half a
+// where the bin is listed; 8 us to look for a bin that is not (128256 logits, half a
 // megabyte, through one compute unit) and 3 to 6 us to find the place in it.
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
 constexpr int kHeld = 1024;     // tokens of one bin that a wave keeps at hand

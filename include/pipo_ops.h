@@ -433,7 +433,7 @@ pipo_status pipo_op_kv8_pages_copy(const pipo_kv8_pages* cache, const int32_t* p
 /*
  * What attention makes of a score x = q . k, and which keys a row sees (NULL, or all
  * zero: x itself, and the keys up to the row's position).  In this order:
- *   cap > 0:    x becomes cap * tanh(x / cap);
+ *   cap > 0:    (2^-126 to 1e30) x becomes cap * tanh(x / cap);
  *   slopes:     (device fp32 [n_heads], NULL: none) slopes[h] * |row's position - key's| is
  *               taken from it;
  *   window > 0: of the keys up to its position a row sees the last `window` alone;

@@ -213,3 +213,31 @@ def test_logits_far_from_zero_and_apart():
                                  -2.0 ** 20, -2.0 ** 21, -1e9, -65.0, -33.0)):
             x[i, rng.integers(0, V, 400)] = min(far, base - abs(far) * 1e-3) if far != -np.inf else far
         check_draw(x, rng.random(rows), T=np.full(rows, T))
+
+
+@BOTH
+@pytest.mark.parametrize("rows", [[1, 1], [80, 33]])
+@pytest.mark.parametrize("cap", [2.0 ** -126, 1e-3, 0.7, 2000.0, 1e6, 1e30])
+def test_caps_of_any_size(cap, rows, fmt):
+    """A cap far above the scores leaves them as they are, one far below makes all weights equal.
+    A capped score is off by some 2^-24 of itself where it is below a quarter of the cap, else by
+    some 2^-24 of the cap, which is at most four times the score: 2^-21 of the smaller of the two
+    bounds that this leaves."""
+    print(f"cap={cap} rows={rows} {fmt}", flush=True)
+    rng = np.random.default_rng(24)
+    lens, H = [300, 47], 2
+    c = Cache(lens, 1, 64, 16, fmt, rng)
+    c.fill(rng)
+    q = draw_q(rng, sum(rows), H, 64, 6.0)
+    got = attend(c, q, rows, H, cap=cap)[:len(q)]
+    want, _ = want_attention(c, q, rows, lens, H, cap=cap)
+    at, tol = 0, np.zeros(want.shape)
+    for i, (r, n) in enumerate(zip(rows, lens)):
+        x = np.abs(q[at:at + r].reshape(r, H, 64).astype(np.float64))
+        k, v = np.abs(c.k[i].values()[:, 0]), np.abs(c.v[i].values())
+        most = max((x[:, h] @ k.T).max() for h in range(H))
+        step = 64 * 2.0 ** -24 * most + 2.0 ** -21 * min(cap, 4 * most) + 2.0 ** -22 * min(most, cap)
+        tol[at:at + r] = (HALF * np.abs(want[at:at + r]) +
+                          (2 * step + (HALF if max(rows) * H > 64 else 2.0 ** -20)) * v.max() + 2.0 ** -25)
+        at += r
+    check(got, want, tol, f"cap {cap}")

@@ -110,6 +110,13 @@ def test_bad_attention(kw, want):
     assert status(B.pipo_op_attn_kv8_pages, cache(), 0, *a.values()) == want
 
 
+@pytest.mark.parametrize("cap", [1e-45, 2.0 ** -127, 2e30])
+def test_caps_out_of_range(cap):
+    """Caps whose reciprocal is not a number, or near the largest one."""
+    assert status(B.pipo_op_attn_kv8_pages, cache(), 0, scores(cap=cap), P, 4096, P, P, P, 4096, 32, 4, 1,
+                  512, None, 0) == "PIPO_ERR_ARG"
+
+
 def test_attention_workspace():
     c = cache(n_seq=1, table_stride=1024, pool=None, table=None)
     ws = B.pipo_op_attn_kv8_pages_workspace_bytes

@@ -26,7 +26,8 @@ def sample(x: np.ndarray, u: float, T: float = 1.0, top_k: int = 0, top_p: float
     if top_k > 0:
         n = min(n, top_k)
     if min_p > 0:
-        n = min(n, int((w >= min(min_p, 1.0)).sum()))
+        # (of the logarithms: a weight just under 1 rounds to 1)
+        n = min(n, int((z >= np.log(min(min_p, 1.0))).sum()))
     run = np.cumsum(w[:n])
     if top_p < 1:
         n = min(n, int((run < max(top_p, 0.0) * run[-1]).sum()) + 1)

@@ -241,3 +241,23 @@ def test_caps_of_any_size(cap, rows, fmt):
                           (2 * step + (HALF if max(rows) * H > 64 else 2.0 ** -20)) * v.max() + 2.0 ** -25)
         at += r
     check(got, want, tol, f"cap {cap}")
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+def test_settings_at_their_ends(workspace):
+    """Temperatures down to the least number, shares and limits of 0 and 1 and one step from them."""
+    rng = np.random.default_rng(25)
+    V, T = 5000, np.repeat(np.array([1e-45, 1e-38, 1e-30, 1e-4, 0.05, 40.0, 3e38], np.float32), 4)
+    rows = len(T)
+    x = (rng.standard_normal((rows, V)) * 2).astype(np.float32)
+    for i in range(0, rows, 2):      # (equal largest logits)
+        x[i, rng.permutation(V)[:7]] = 9.0
+    u = np.tile(np.array([0.0, 0.3, 0.9, 1 - 2.0 ** -24], np.float32), rows // 4)
+    check_draw(x, u, T=T, workspace=workspace)
+    below, least = 1 - 2.0 ** -24, 2.0 ** -126
+    for p in (0.0, least, 0.5, below):
+        check_draw(x, u, T=T, p=np.full(rows, p), workspace=workspace)
+    for m in (least, 0.5, below, 1.0, 7.0):
+        check_draw(x, u, T=T, m=np.full(rows, m), workspace=workspace)
+    for k in (-1, 1, 7, 8, V - 1, V, 2 ** 31 - 1):
+        check_draw(x, u, T=T, k=np.full(rows, k), p=np.full(rows, 0.7), workspace=workspace)

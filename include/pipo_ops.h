@@ -456,7 +456,8 @@ typedef struct {
  * Of the table, a sequence's entries up to position max_len may be read.  A row that sees
  * no key becomes 0.  Keys and values are read exactly, softmax and
  * sums in fp32, the output rounded once to fp16; where a sequence may have more than
- * 64 rows times query heads of a key/value head, weights are rounded to fp16 as well.
+ * 16 rows times query heads of a key/value head, weights may be rounded to fp16 as well
+ * (above 64 they are).
  */
 pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* cache, int32_t layer,
                                    const pipo_attn_scores* scores, const uint16_t* q, int64_t ldq,

@@ -32,8 +32,9 @@ struct Attn8 {
   bool q_vec, o_vec;
 };
 
-// Up to this many columns a sequence is attn8_few_k's, above it attn8_many_k's; all of them
-// where every row of the call may be one of max_q equal shares, which saves a launch.
+// Up to Plan8::few_cols columns, this many at most, a sequence is attn8_few_k's, above them
+// attn8_many_k's; all of them where every row of the call may be one of max_q equal shares,
+// which saves a launch.
 constexpr int kFewCols = 64;
 constexpr int kBlock = 32;      // keys that a wave of few columns takes at a time
 constexpr int kManyCols = 128, kManyKeys = 64;
@@ -931,6 +932,10 @@ static int chunk_of(int64_t keys, int64_t S, int block) {
 
 // Splits and shares, by sizes alone, measured on both sides (us, 8 heads of 128, 4 query heads
 // each unless said):
+//   few_cols: keys are read anew for each 16 columns, so as many as two workgroups a CU have:
+//          16 rows of 16 sequences over 2000 keys 32.1, as many columns 33.5; of 32 81.9
+//          and 45.4; 8 rows of 32 43.5 and 44.2; of 64 86.7 and 61.7 (one sequence of 12 rows
+//          and 500 keys 8.9 and 15.6);
 //   waves: 8 where workgroups are up to one a CU (16 sequences 17.5, by 4 waves 18.7; but 32
 //          in a window 16.6 and 15.5), else 4, two workgroups a CU and no more (64 of 56
 //          heads 79, by 8 waves 107 to 111; 64 of 8 heads 45 and 47);
@@ -942,6 +947,7 @@ static int chunk_of(int64_t keys, int64_t S, int block) {
 //          up to 4099 keys 96, by one team 118), else 1 (8 of 512 rows 41, by two 61).
 constexpr int kCUs = 256, kMinFew = 256, kSplitFew = 768, kMinMany = 512;
 struct Plan8 {
+  int few_cols;     // of a sequence, at most, that is of the first kind
   bool few, many;   // sequences that may be of either kind
   int waves;        // of a workgroup for those of few columns
   int teams;        // of a workgroup for the others
@@ -953,18 +959,19 @@ static Plan8 plan_attn8(const pipo_kv8_pages* c, const pipo_attn_scores* f, int 
                         int64_t max_q, int64_t max_len) {
   const int G = n_heads / c->n_kv_heads;
   Plan8 p;
-  p.many = max_q * G > kFewCols;
-  p.few = !p.many || (G <= kFewCols && M < c->n_seq * max_q);
-  const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, kFewCols / G));
+  p.few_cols = (int)std::min<int64_t>(kFewCols, 16 * std::max<int64_t>(1, 2 * kCUs / ((int64_t)c->n_seq * c->n_kv_heads)));
+  p.many = max_q * G > p.few_cols;
+  p.few = !p.many || (G <= p.few_cols && M < c->n_seq * max_q);
+  const int64_t few_q = std::max<int64_t>(1, std::min<int64_t>(max_q, p.few_cols / G));
   // (with many columns about, most of the others have one row)
   const int64_t q = p.many ? 1 : few_q, wgs = (int64_t)c->n_seq * c->n_kv_heads * col_tiles(q, G, 16);
   const int64_t few = seen_keys(f, few_q, max_len, kBlock), many = seen_keys(f, max_q, max_len, kManyKeys);
   p.waves = wgs <= kCUs ? 8 : 4;
   p.chunk_few = chunk_of(few, few < kSplitFew ? 1 : std::min(kCUs / wgs, few / kMinFew), kBlock);
   p.tiles = std::min(c->n_seq * col_tiles(max_q, G, kManyCols), M * G / kManyCols + c->n_seq);
-  // (of n columns above 64, at most n / 64.5)
+  // (of n columns above few_cols, at most n / (few_cols + 1), and n / 64.5)
   static_assert(kManyCols == 2 * kFewCols, "the bound of a sequence's tiles");
-  if (p.few) p.tiles = std::min(p.tiles, 2 * M * G / 129);
+  if (p.few) p.tiles = std::min(p.tiles, p.few_cols < kFewCols ? M * G / (p.few_cols + 1) : 2 * M * G / 129);
   const int64_t tiles = std::max<int64_t>(1, p.tiles * c->n_kv_heads);
   p.chunk_many = chunk_of(many, std::min((kCUs + tiles - 1) / tiles, many / kMinMany), kManyKeys);
   if (M >= (1 << 23)) {   // (a grid of M workgroups)
@@ -1009,7 +1016,7 @@ static pipo_status check_attn8(const char* what, const pipo_kv8_pages* c, const 
 template <int D, bool INT8, bool MOD>
 static void launch_attn8(const Attn8& a, const Plan8& p, hipStream_t st) {
   if (p.few) {
-    const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, p.many ? kFewCols : INT32_MAX);
+    const int64_t cols = std::min<int64_t>((int64_t)a.max_q * a.G, p.many ? p.few_cols : INT32_MAX);
     const dim3 g((unsigned)(a.c.Hkv * a.c.n_seq), (unsigned)p.splits_few, (unsigned)((cols + 15) / 16));
     if (p.waves == 8)
       launch(attn8_few_k<D, INT8, MOD, 8>, g, dim3(512), 0, st, a);
@@ -1088,7 +1095,7 @@ pipo_status pipo_op_attn_kv8_pages(const pipo_kv8_pages* c, int32_t layer, const
     p.chunk_few = p.chunk_many = std::max(kManyKeys, (max_len + kManyKeys - 1) / kManyKeys * kManyKeys);
     p.splits_few = p.splits_many = 1;
   }
-  a.few_cols = p.few ? kFewCols : 0;
+  a.few_cols = p.few ? p.few_cols : 0;
   a.chunk_few = p.chunk_few;
   a.chunk_many = p.chunk_many;
   a.splits = p.splits();

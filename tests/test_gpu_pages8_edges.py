@@ -261,3 +261,20 @@ def test_settings_at_their_ends(workspace):
         check_draw(x, u, T=T, m=np.full(rows, m), workspace=workspace)
     for k in (-1, 1, 7, 8, V - 1, V, 2 ** 31 - 1):
         check_draw(x, u, T=T, k=np.full(rows, k), p=np.full(rows, 0.7), workspace=workspace)
+
+
+@BOTH
+@pytest.mark.parametrize("n,H,Hkv", [(70, 16, 4), (33, 32, 8), (300, 4, 2), (60, 16, 4), (40, 16, 4)])
+def test_some_rows_of_many_sequences(n, H, Hkv, fmt):
+    """Sequences of 1 to 17 rows, in batches large enough to be taken by 128 columns from 17, 33
+    or 49 columns on: columns at each of these numbers.  (17 rows of 4 heads: any weights may be
+    rounded.)"""
+    print(f"some rows n={n} H={H}/{Hkv} {fmt}", flush=True)
+    rng = np.random.default_rng(n)
+    G = H // Hkv
+    some = [1, 1, 4, 5, 8, 9, 12, 13, 16, 17] if G == 4 else [1, 8, 9, 16, 17, 24, 25, 32, 33]
+    for biggest in (some[-1], 4):
+        rows = [int(x) for x in rng.choice([r for r in some if r <= biggest], n)]
+        rows[n // 2] = biggest
+        lens = [r + int(x) for r, x in zip(rows, rng.integers(0, 150, n))]
+        run_attention(lens, rows, H, Hkv, 64, 16, fmt, slopes=n == 33, window=50 if n == 70 else 0)
